@@ -250,6 +250,78 @@ d2mhe_status d2mhe_round_group_static(d2mhe_ctx *ctx, const uint64_t *pk,
 d2mhe_status d2mhe_average_update(const float *sum, uint32_t K, const float *grad, float gamma,
                                   uint64_t n, float *w, void *stream);
 
+/* ---- exchange of answers: the float work before and after a round ------------------------------ */
+/* A neighbourhood can exchange what its models answer on shared examples instead of their weights:
+ * for every example the log-probabilities of k classes are encoded, encrypted, summed and decrypted
+ * like any other vector (rows * k values, see d2mhe_round), and every node moves its model towards
+ * the mean.  The positions (class indices) travel in the clear, the answers encrypted.  An iteration:
+ *   one node      d2mhe_top_logprobs   chooses the positions
+ *   every member  d2mhe_logprobs_at    answers there: the vector for the round
+ *   every node    d2mhe_distill        loss against the decoded sum, and its gradient
+ * These calls need no context.  No call changes its inputs; sums, maxima and row statistics are held
+ * in 32 bits, only a gradient is rounded to the type of the logits, once.  Results do not depend on
+ * the launch: the same call gives the same bits.  The two descriptors are HOST memory that a call has
+ * read when it returns; the pointers they hold are device pointers.  Outputs may overlap neither
+ * inputs nor the scratch.                                                                        */
+enum { D2MHE_F32 = 0, D2MHE_F16 = 1, D2MHE_BF16 = 2 };
+#define D2MHE_MAX_TOP 256u
+
+typedef struct {
+    const void *logits;   /* row r: `classes` values from element r * row_stride on; the elements
+                             between the rows are not used.  -inf excludes a class; a NaN or +inf
+                             makes the results of its row NaN (the positions stay defined)       */
+    uint32_t dtype;       /* D2MHE_F32, D2MHE_F16 or D2MHE_BF16                                  */
+    uint32_t rows;        /* 0 .. 2^31 - 1; 0: no-op                                             */
+    uint32_t classes;     /* 1 .. 2^31 - 1                                                       */
+    uint64_t row_stride;  /* in elements, >= classes, any alignment; rows * row_stride < 2^60    */
+} d2mhe_logits;
+
+typedef struct {
+    const int32_t *index; /* [rows][k] class of every slot; a value outside 0 .. classes - 1 is an
+                             empty slot, and what `sum` holds there is not used                  */
+    const float *sum;     /* [rows][k] decoded sum of the members' log-probabilities             */
+    const float *weight;  /* [rows] factor of the row's loss (times an incoming gradient, if there
+                             is one); 0: the row is padding; NULL: 1 for all                     */
+    uint32_t k;           /* 1 .. D2MHE_MAX_TOP                                                  */
+    uint32_t members;     /* K >= 1: the mean answer is sum / K                                  */
+    float temperature;    /* 0.01 .. 100                                                         */
+} d2mhe_teacher;
+
+/* Bytes of scratch that d2mhe_top_logprobs, d2mhe_logprobs_at and d2mhe_distill need for these logits
+ * and k (a positive multiple of 256; 0 if the descriptor is invalid; its pointer is not looked at).
+ * Calls that overlap in time need a scratch each, graphs that are replayed side by side as well. */
+size_t d2mhe_logits_scratch_bytes(const d2mhe_logits *z, uint32_t k);
+/* The k largest logits of every row in decreasing order (among equals the lower class first; -0 and
+ * +0 are equal), index [rows][k], and their log-probabilities z - log sum exp z, logprob [rows][k].
+ * Logits of -inf and NaN are never chosen: slots left over hold index -1 and logprob 0.         */
+d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *index, float *logprob,
+                                void *scratch, size_t scratch_bytes, void *stream);
+/* logprob [rows][k] = z - log sum exp z at the classes index [rows][k], in any order, any of them more
+ * than once; 0 in empty slots (an index outside 0 .. classes - 1).  The log-probability of a -inf
+ * logit is -inf, which the encoders clamp to their least value.                                  */
+d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint32_t k, float *logprob,
+                               void *scratch, size_t scratch_bytes, void *stream);
+/* Distillation towards the mean answer s_j = sum_j / members of the filled slots j of a row, at
+ * temperature T: with p = softmax_j(s_j / T) (equal to softmax over these classes alone) and
+ * lse = log sum_v exp(z_v / T) over all classes v,
+ *   loss = weight * sum_j p_j (log p_j - (z_{index_j} / T - lse)),
+ *   grad_v = weight / T * (exp(z_v / T - lse) - sum_{j: index_j = v} p_j)    (d loss / d z_v).
+ * loss, lse [rows]; grad: type of the logits, row r from element r * grad_stride on
+ * (grad_stride >= classes; the elements between the rows are left as they are); NULL: no gradient.
+ * A teacher's sum of -inf counts as probability 0.  Rows of weight 0 and rows without a filled slot of
+ * a sum above -inf give loss, lse and gradient 0, and their logits are not used; rows whose logits are
+ * all -inf give loss and gradient 0 and lse -inf.  The factor T^2 that some add is the caller's, in
+ * `weight`.                                                                                       */
+d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, float *loss, float *lse,
+                           void *grad, uint64_t grad_stride, void *scratch, size_t scratch_bytes,
+                           void *stream);
+/* The gradient of d2mhe_distill alone, from the lse [rows] which that call gave for the same logits and
+ * temperature (a loss whose gradient turns out to be needed later).  A weight other than the one of
+ * the loss is the place for the gradient that arrives at it.  exp(z_v / T - lse) carries lse's rounding:
+ * a relative error of up to 2^-24 |lse|.  Rows with lse -inf give 0.                              */
+d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *teacher, const float *lse,
+                                    void *grad, uint64_t grad_stride, void *stream);
+
 /* ---- MBFV.Convert: key switching to a receiver's own key (Sec. 4.2 item 3) ------------------- */
 /* In the paper's protocol node i does not take part in a collective decryption of the
  * aggregate; the members of its closed neighbourhood switch the aggregate to node i's own

@@ -27,7 +27,11 @@ SYMBOLS = [
     "d2mhe_round_convert_scratch_bytes", "d2mhe_round_convert",
     "d2mhe_bootstrap_alpha", "d2mhe_bootstrap_share", "d2mhe_bootstrap_combine",
     "d2mhe_average_update", "d2mhe_encode_coefficients", "d2mhe_decode_coefficients",
+    "d2mhe_logits_scratch_bytes", "d2mhe_top_logprobs", "d2mhe_logprobs_at", "d2mhe_distill", "d2mhe_distill_backward",
 ]
+
+F32, F16, BF16 = range(3)                # types of logits
+MAX_TOP = 256                            # D2MHE_MAX_TOP of the header
 
 
 class Params(C.Structure):
@@ -49,6 +53,16 @@ class ConvertDesc(C.Structure):
     _fields_ = [("recv_offsets", C.POINTER(C.c_uint32)), ("receivers", C.POINTER(C.c_uint32)),
                 ("recv_pks", C.POINTER(C.c_void_p)), ("recv_sks", C.POINTER(C.c_void_p)),
                 ("out_recv", C.POINTER(C.c_void_p))]
+
+
+class LogitsDesc(C.Structure):
+    _fields_ = [("logits", C.c_void_p), ("dtype", C.c_uint32), ("rows", C.c_uint32), ("classes", C.c_uint32),
+                ("row_stride", C.c_uint64)]
+
+
+class TeacherDesc(C.Structure):
+    _fields_ = [("index", C.c_void_p), ("sum", C.c_void_p), ("weight", C.c_void_p), ("k", C.c_uint32),
+                ("members", C.c_uint32), ("temperature", C.c_float)]
 
 
 class D2mheError(RuntimeError):
@@ -105,6 +119,11 @@ def lib():
         "d2mhe_average_update": (i32, [vp, u32, vp, C.c_float, u64, vp, vp]),
         "d2mhe_encode_coefficients": (i32, [vp, vp, u64, vp, u32, vp]),
         "d2mhe_decode_coefficients": (i32, [vp, vp, u32, u64, vp, vp]),
+        "d2mhe_logits_scratch_bytes": (sz, [C.POINTER(LogitsDesc), u32]),
+        "d2mhe_top_logprobs": (i32, [C.POINTER(LogitsDesc), u32, vp, vp, vp, sz, vp]),
+        "d2mhe_logprobs_at": (i32, [C.POINTER(LogitsDesc), vp, u32, vp, vp, sz, vp]),
+        "d2mhe_distill": (i32, [C.POINTER(LogitsDesc), C.POINTER(TeacherDesc), vp, vp, vp, u64, vp, sz, vp]),
+        "d2mhe_distill_backward": (i32, [C.POINTER(LogitsDesc), C.POINTER(TeacherDesc), vp, vp, u64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -141,6 +160,46 @@ def make_params(log2_n, q, t, cbd_eta=21, frac_bits=0, max_group=1, seed=0):
 
 def average_update(sum_, K, grad, gamma, n, w, stream=None):
     _check(lib().d2mhe_average_update(_ptr(sum_), K, _ptr(grad), gamma, n, _ptr(w), stream), "d2mhe_average_update")
+
+
+# ---- exchange of answers ----
+def make_logits(logits, dtype, rows, classes, row_stride=None):
+    """Describe rows of logits (F32, F16 or BF16) for the calls below; row_stride in elements, None: rows without gaps."""
+    d = LogitsDesc(_ptr(logits), dtype, rows, classes, classes if row_stride is None else row_stride)
+    d._keep = logits
+    return d
+
+
+def make_teacher(index, sum_, k, members, temperature=1.0, weight=None):
+    """Describe a neighbourhood's answers: positions [rows][k] (int32), their decoded sums over `members` nodes, and a
+    factor for every row's loss (None: 1)."""
+    d = TeacherDesc(_ptr(index), _ptr(sum_), _ptr(weight), k, members, temperature)
+    d._keep = (index, sum_, weight)
+    return d
+
+
+def logits_scratch_bytes(z, k):
+    return lib().d2mhe_logits_scratch_bytes(C.byref(z), k)
+
+
+def top_logprobs(z, k, index, logprob, scratch, scratch_bytes, stream=None):
+    _check(lib().d2mhe_top_logprobs(C.byref(z), k, _ptr(index), _ptr(logprob), _ptr(scratch), scratch_bytes, stream),
+           "d2mhe_top_logprobs")
+
+
+def logprobs_at(z, index, k, logprob, scratch, scratch_bytes, stream=None):
+    _check(lib().d2mhe_logprobs_at(C.byref(z), _ptr(index), k, _ptr(logprob), _ptr(scratch), scratch_bytes, stream),
+           "d2mhe_logprobs_at")
+
+
+def distill(z, teacher, loss, lse, grad, grad_stride, scratch, scratch_bytes, stream=None):
+    _check(lib().d2mhe_distill(C.byref(z), C.byref(teacher), _ptr(loss), _ptr(lse), _ptr(grad), grad_stride, _ptr(scratch),
+                               scratch_bytes, stream), "d2mhe_distill")
+
+
+def distill_backward(z, teacher, lse, grad, grad_stride, stream=None):
+    _check(lib().d2mhe_distill_backward(C.byref(z), C.byref(teacher), _ptr(lse), _ptr(grad), grad_stride, stream),
+           "d2mhe_distill_backward")
 
 
 def workspace_bytes(params: Params) -> int:

@@ -1,0 +1,135 @@
+// C-ABI entry points of the exchange of answers (see include/d2mhe.h): argument checks and launches.
+#include "answers.hpp"
+
+using namespace d2::answers;
+
+namespace {
+
+bool misaligned(const void *p) { return ((uintptr_t)p & 15u) != 0; }
+
+uint64_t word(uint32_t dtype) { return dtype == D2MHE_F32 ? 4 : 2; }
+
+bool valid(const d2mhe_logits *z)
+{
+    return z->dtype <= D2MHE_BF16 && z->rows < (1u << 31) && z->classes >= 1 && z->classes < (1u << 31) &&
+           z->row_stride >= z->classes && (z->rows == 0 || z->row_stride < (1ull << 60) / z->rows);
+}
+
+bool valid_k(uint32_t k) { return k >= 1 && k <= MAX_TOP; }
+
+bool valid(const d2mhe_teacher *t)
+{
+    return valid_k(t->k) && t->members >= 1 && t->temperature >= 0.01f && t->temperature <= 100.0f;
+}
+
+// bytes from the first to behind the last used element
+uint64_t span(uint64_t rows, uint64_t stride, uint64_t used, uint64_t bytes) { return ((rows - 1) * stride + used) * bytes; }
+
+bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb)
+{
+    return (uintptr_t)a < (uintptr_t)b + nb && (uintptr_t)b < (uintptr_t)a + na;
+}
+
+d2mhe_status check_gradient(const d2mhe_logits *z, const void *grad, uint64_t stride)
+{
+    if (stride < z->classes || (z->rows && stride >= (1ull << 60) / z->rows)) return D2MHE_ERR_RANGE;
+    if (misaligned(grad)) return D2MHE_ERR_ALIGN;
+    const uint64_t b = word(z->dtype);
+    if (z->rows && overlap(z->logits, span(z->rows, z->row_stride, z->classes, b), grad, span(z->rows, stride, z->classes, b)))
+        return D2MHE_ERR_RANGE;
+    return D2MHE_OK;
+}
+
+Rows rows_of(const d2mhe_logits *z) { return {z->logits, z->row_stride, z->rows, z->classes}; }
+
+Answers answers_of(const d2mhe_teacher *t)
+{
+    return {t->index, t->sum, t->weight, t->k, 1.0f / (float)t->members, 1.0f / t->temperature};
+}
+
+// f(T()) with the element type of the logits
+template <class F> d2mhe_status with_type(uint32_t dtype, F f)
+{
+    if (dtype == D2MHE_F32) f(float());
+    else if (dtype == D2MHE_F16) f((_Float16)0);
+    else f((__bf16)0.0f);
+    return hipGetLastError() == hipSuccess ? D2MHE_OK : D2MHE_ERR_HIP;
+}
+
+unsigned grid_of(uint32_t rows) { return rows < (1u << 20) ? rows : 1u << 20; }
+
+}  // namespace
+
+extern "C" {
+
+size_t d2mhe_logits_scratch_bytes(const d2mhe_logits *z, uint32_t k)
+{
+    if (!z || !valid(z) || !valid_k(k)) return 0;
+    return 256;
+}
+
+d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *index, float *logprob, void *scratch,
+                                size_t scratch_bytes, void *stream)
+{
+    if (!z || !z->logits || !index || !logprob || !scratch) return D2MHE_ERR_NULL;
+    if (!valid(z) || !valid_k(k)) return D2MHE_ERR_RANGE;
+    if (misaligned(z->logits) || misaligned(index) || misaligned(logprob) || misaligned(scratch)) return D2MHE_ERR_ALIGN;
+    if (scratch_bytes < d2mhe_logits_scratch_bytes(z, k)) return D2MHE_ERR_WORKSPACE;
+    if (z->rows == 0) return D2MHE_OK;
+    return with_type(z->dtype, [&](auto zero) {
+        hipLaunchKernelGGL(k_top<decltype(zero)>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream, rows_of(z), k,
+                           index, logprob);
+    });
+}
+
+d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint32_t k, float *logprob, void *scratch,
+                               size_t scratch_bytes, void *stream)
+{
+    if (!z || !z->logits || !index || !logprob || !scratch) return D2MHE_ERR_NULL;
+    if (!valid(z) || !valid_k(k)) return D2MHE_ERR_RANGE;
+    if (misaligned(z->logits) || misaligned(index) || misaligned(logprob) || misaligned(scratch)) return D2MHE_ERR_ALIGN;
+    if (scratch_bytes < d2mhe_logits_scratch_bytes(z, k)) return D2MHE_ERR_WORKSPACE;
+    if (z->rows == 0) return D2MHE_OK;
+    return with_type(z->dtype, [&](auto zero) {
+        hipLaunchKernelGGL(k_logprobs_at<decltype(zero)>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream,
+                           rows_of(z), index, k, logprob);
+    });
+}
+
+d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, float *loss, float *lse, void *grad,
+                           uint64_t grad_stride, void *scratch, size_t scratch_bytes, void *stream)
+{
+    if (!z || !teacher || !z->logits || !teacher->index || !teacher->sum || !loss || !lse || !scratch) return D2MHE_ERR_NULL;
+    if (!valid(z) || !valid(teacher)) return D2MHE_ERR_RANGE;
+    if (misaligned(z->logits) || misaligned(teacher->index) || misaligned(teacher->sum) || misaligned(teacher->weight) ||
+        misaligned(loss) || misaligned(lse) || misaligned(scratch))
+        return D2MHE_ERR_ALIGN;
+    if (grad)
+        if (d2mhe_status s = check_gradient(z, grad, grad_stride)) return s;
+    if (scratch_bytes < d2mhe_logits_scratch_bytes(z, teacher->k)) return D2MHE_ERR_WORKSPACE;
+    if (z->rows == 0) return D2MHE_OK;
+    return with_type(z->dtype, [&](auto zero) {
+        using T = decltype(zero);
+        hipLaunchKernelGGL(k_distill<T>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream, rows_of(z),
+                           answers_of(teacher), loss, lse, (T *)grad, grad_stride);
+    });
+}
+
+d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *teacher, const float *lse, void *grad,
+                                    uint64_t grad_stride, void *stream)
+{
+    if (!z || !teacher || !z->logits || !teacher->index || !teacher->sum || !lse || !grad) return D2MHE_ERR_NULL;
+    if (!valid(z) || !valid(teacher)) return D2MHE_ERR_RANGE;
+    if (misaligned(z->logits) || misaligned(teacher->index) || misaligned(teacher->sum) || misaligned(teacher->weight) ||
+        misaligned(lse))
+        return D2MHE_ERR_ALIGN;
+    if (d2mhe_status s = check_gradient(z, grad, grad_stride)) return s;
+    if (z->rows == 0) return D2MHE_OK;
+    return with_type(z->dtype, [&](auto zero) {
+        using T = decltype(zero);
+        hipLaunchKernelGGL(k_distill_backward<T>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream, rows_of(z),
+                           answers_of(teacher), lse, (T *)grad, grad_stride);
+    });
+}
+
+}  // extern "C"

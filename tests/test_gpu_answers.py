@@ -1,0 +1,435 @@
+"""Top classes, log-probabilities at given classes, distillation loss and gradient on the GPU against their formulas in
+64 bits (tests/answers_ref.py, which also derives the tolerances)."""
+import numpy as np
+import pytest
+import torch
+
+import answers_ref as R
+from paper_2207_04604_amd import binding as B
+
+from gpu_util import DEV
+
+pytestmark = pytest.mark.gpu
+
+TORCH = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+CODE = {"f32": B.F32, "f16": B.F16, "bf16": B.BF16}
+HALF_STEP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}          # finfo.eps / 2
+LEAST = {"f32": 2.0 ** -126, "f16": 2.0 ** -25, "bf16": 2.0 ** -126}            # half a subnormal step; exp2 flushes below 2^-126
+GUARD = 1234.0
+
+# rows, classes, elements between rows, k: one class; fewer classes than slots; around a wavefront, a workgroup and a
+# 16-byte word; odd strides; the largest k; rows longer than what a workgroup can hold
+SHAPES = [(1, 1, 0, 1), (3, 2, 0, 5), (256, 10, 0, 10), (5, 63, 1, 7), (67, 64, 0, 64), (5, 65, 3, 65), (700, 257, 0, 3),
+          (9, 511, 0, 100), (4, 1000, 24, 17), (33, 1023, 2, 256), (3, 2049, 0, 33), (2, 4099, 5, 250), (5, 8192, 0, 8),
+          (2, 12289, 0, 64), (3, 32769, 0, 64), (1, 50001, 0, 16), (40, 50001, 0, 5), (2, 131072, 0, 256), (3, 131081, 7, 31),
+          (1, 300007, 0, 64), (600, 20011, 0, 3)]
+
+
+def logits(rng, rows, V, pad, dtype, spread=3.0):
+    """A device buffer [rows][V + pad] and its values in 64 bits; between the rows there is no number."""
+    z = torch.from_numpy(rng.normal(0, spread, (rows, V)).astype(np.float32)).to(TORCH[dtype])
+    buf = torch.full((rows, V + pad), float("nan"), dtype=TORCH[dtype], device=DEV)
+    buf[:, :V] = z.to(DEV)
+    return buf, z.double().numpy()
+
+
+def describe(buf, dtype, V):
+    return B.make_logits(buf, CODE[dtype], buf.shape[0], V, row_stride=buf.shape[1])
+
+
+def scratch_for(z, k):
+    n = B.logits_scratch_bytes(z, k)
+    return torch.full((n // 8,), -1, dtype=torch.int64, device=DEV), n
+
+
+def slots(rng, rows, V, k, empty=0.0, twice=False):
+    index = np.stack([rng.permutation(V)[:k] if V >= k else np.r_[rng.permutation(V), np.full(k - V, -1)] for _ in range(rows)])
+    if twice:
+        index[:, k // 2:] = index[:, :k - k // 2]
+    index[rng.random(index.shape) < empty] = rng.choice([-1, V, 2 ** 31 - 1, -2 ** 31])
+    return index.astype(np.int32)
+
+
+def answers(rng, rows, k, members):
+    return (-np.rint(rng.random((rows, k)) * 6 * members * 256) / 256).astype(np.float32)
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+
+
+def run_top(buf, dtype, V, k, stream=None):
+    rows = buf.shape[0]
+    z = describe(buf, dtype, V)
+    index = torch.full((rows + 1, k), 77, dtype=torch.int32, device=DEV)
+    lp = torch.full((rows + 1, k), GUARD, device=DEV)
+    s, n = scratch_for(z, k)
+    B.top_logprobs(z, k, index, lp, s, n, stream)
+    torch.cuda.synchronize()
+    assert (index[rows] == 77).all() and (lp[rows] == GUARD).all()
+    return index[:rows].cpu().numpy(), lp[:rows].cpu().numpy().astype(np.float64)
+
+
+def run_at(buf, dtype, V, index, stream=None):
+    rows, k = index.shape
+    z = describe(buf, dtype, V)
+    lp = torch.full((rows + 1, k), GUARD, device=DEV)
+    s, n = scratch_for(z, k)
+    B.logprobs_at(z, dev(index), k, lp, s, n, stream)
+    torch.cuda.synchronize()
+    assert (lp[rows] == GUARD).all()
+    return lp[:rows].cpu().numpy().astype(np.float64)
+
+
+def run_distill(buf, dtype, V, index, sums, members, T, weight=None, gap=0, grad=True, lse=None, stream=None):
+    """(loss, lse, gradient) of distill, or the gradient of distill_backward for a given lse"""
+    rows, k = index.shape
+    z = describe(buf, dtype, V)
+    keep = dev(index), dev(sums), dev(weight) if weight is not None else None
+    t = B.make_teacher(keep[0], keep[1], k, members, T, keep[2])
+    g = torch.full((rows + 1, V + gap), GUARD, dtype=TORCH[dtype], device=DEV)
+    if lse is not None:
+        held = dev(lse)
+        B.distill_backward(z, t, held, g, V + gap, stream)
+        torch.cuda.synchronize()
+        guarded(g, rows, V)
+        return g[:rows, :V].double().cpu().numpy()
+    loss, out = torch.full((rows + 1,), GUARD, device=DEV), torch.full((rows + 1,), GUARD, device=DEV)
+    s, n = scratch_for(z, k)
+    B.distill(z, t, loss, out, g if grad else None, V + gap, s, n, stream)
+    torch.cuda.synchronize()
+    assert loss[rows] == GUARD and out[rows] == GUARD
+    guarded(g, rows if grad else 0, V)
+    return (loss[:rows].cpu().numpy(), out[:rows].cpu().numpy(), g[:rows, :V].double().cpu().numpy() if grad else None)
+
+
+def guarded(g, rows, V):
+    assert (g[:rows, V:] == GUARD).all() and (g[rows:] == GUARD).all()
+
+
+def within(got, want, error):
+    bad = ~(np.abs(got - want) <= error)
+    assert not bad.any(), (np.argwhere(bad)[:3], got[bad][:3], want[bad][:3], np.broadcast_to(error, bad.shape)[bad][:3])
+
+
+# ---- the formulas -----------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_top_logprobs(shape, dtype):
+    rows, V, pad, k = shape
+    buf, z = logits(np.random.default_rng(V + k), rows, V, pad, dtype)
+    index, lp = run_top(buf, dtype, V, k)
+    want, wlp = R.top_logprobs(z, k)
+    assert np.array_equal(index, want)
+    within(lp, wlp, R.logprob_error(z, wlp))
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_logprobs_at(shape, dtype):
+    rows, V, pad, k = shape
+    rng = np.random.default_rng(V + 2 * k)
+    buf, z = logits(rng, rows, V, pad, dtype)
+    index = slots(rng, rows, V, k, empty=0.1, twice=True)
+    want = R.logprobs_at(z, index)
+    within(run_at(buf, dtype, V, index), want, R.logprob_error(z, want))
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("shape", SHAPES, ids=str)
+def test_distill(shape, dtype):
+    """Loss, lse and gradient; the loss alone; the gradient alone from the lse. Slots are empty, rows padded."""
+    rows, V, pad, k = shape
+    rng = np.random.default_rng(V + 3 * k)
+    buf, z = logits(rng, rows, V, pad, dtype)
+    members, T = 5, [1.0, 2.0, 0.7][(V + k) % 3]
+    index, sums = slots(rng, rows, V, k, empty=0.1), answers(rng, rows, k, members)
+    weight = rng.choice([0.0, 0.25, 1.0, -2.0], rows, p=[0.1, 0.4, 0.4, 0.1]).astype(np.float32)
+    d = R.Distill(z, index, sums, members, T, weight)
+    for gap in ([0, 3] if V < 3000 else [(V + k) % 2 * 5]):
+        loss, lse, grad = run_distill(buf, dtype, V, index, sums, members, T, weight, gap=gap)
+        within(loss, d.loss, d.loss_error)
+        within(lse, d.lse, d.lse_error)
+        within(grad, d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+        loss2, lse2, _ = run_distill(buf, dtype, V, index, sums, members, T, weight, grad=False)
+        within(loss2, d.loss, d.loss_error)
+        within(lse2, d.lse, d.lse_error)
+        grad = run_distill(buf, dtype, V, index, sums, members, T, weight, gap=gap, lse=lse)
+        d2 = R.Distill(z, index, sums, members, T, weight, lse=lse)
+        within(grad, d2.grad, d2.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+
+
+@pytest.mark.parametrize("shape", [(5, 65, 3, 65), (3, 2049, 0, 32), (2, 40000, 0, 256), (2, 131081, 7, 31)], ids=str)
+def test_a_class_in_several_slots(shape):
+    rows, V, pad, k = shape
+    rng = np.random.default_rng(V)
+    buf, z = logits(rng, rows, V, pad, "f32")
+    index, sums = slots(rng, rows, V, k, twice=True), answers(rng, rows, k, 3)
+    index[0] = index[0, 0]                                          # one class in all slots
+    d = R.Distill(z, index, sums, 3, 1.0)
+    loss, lse, grad = run_distill(buf, "f32", V, index, sums, 3, 1.0)
+    within(loss, d.loss, d.loss_error)
+    within(grad, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+    d = R.Distill(z, index, sums, 3, 1.0, lse=lse)
+    within(run_distill(buf, "f32", V, index, sums, 3, 1.0, lse=lse), d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+
+
+def test_gradient_is_that_of_the_loss():
+    """Central differences of the loss in 64 bits: their own error is h^2 / 6 times the third derivative of the
+    log-sum-exp (at most 1 / T^3 in absolute value), plus its rounding (1e-14 / h)."""
+    rng = np.random.default_rng(5)
+    rows, V, k, members, T, h = 3, 37, 9, 4, 1.5, 1e-4
+    buf, z = logits(rng, rows, V, 0, "f32")
+    index, sums = slots(rng, rows, V, k, empty=0.2), answers(rng, rows, k, members)
+    weight = np.array([1.0, 0.5, 0.0], np.float32)
+    _, _, grad = run_distill(buf, "f32", V, index, sums, members, T, weight)
+    d = R.Distill(z, index, sums, members, T, weight)
+    for v in range(V):
+        step = np.zeros((rows, V))
+        step[:, v] = h
+        diff = (R.Distill(z + step, index, sums, members, T, weight).loss -
+                R.Distill(z - step, index, sums, members, T, weight).loss) / (2 * h)
+        within(grad[:, v], diff, h * h / 6 / T ** 3 + 1e-14 / h * 10 + d.grad_error[:, v] + 2 * R.U * np.abs(diff))
+
+
+# ---- values at the ends -----------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("V,k", [(9, 4), (100, 20), (1000, 100), (5000, 256), (131072, 64)])
+def test_equal_logits_go_to_the_lower_class(dtype, V, k):
+    rng = np.random.default_rng(V)
+    z = rng.integers(-2, 3, (6, V)).astype(np.float32)              # few values, so nearly all are ties
+    z[1] = 0.5                                                     # one value
+    z[2] = np.where(rng.random(V) < 0.5, 0.0, -0.0)                # equal zeros
+    z[3] = np.sort(z[3])
+    z[4] = -np.sort(-z[4])
+    z[5] = -7.0
+    z[5, -3:] = [-8.0, 1.0, 1.0]
+    buf = torch.from_numpy(z).to(TORCH[dtype]).to(DEV)
+    index, lp = run_top(buf, dtype, V, k)
+    want, wlp = R.top_logprobs(z.astype(np.float64), k)
+    assert np.array_equal(index, want)
+    within(lp, wlp, R.logprob_error(z, wlp))
+
+
+@pytest.mark.parametrize("V,k", [(40, 12), (3000, 256), (70000, 100)])
+def test_all_large_logits_side_by_side(V, k):
+    """Increasing and decreasing rows, and rows whose large values all lie in one short run or a fixed distance apart."""
+    rng = np.random.default_rng(V)
+    z = np.zeros((5, V), np.float32)
+    z[0] = np.arange(V) * 1e-3
+    z[1] = -np.arange(V) * 1e-3
+    z[2, V // 2:V // 2 + k] = 5 + rng.random(min(k, V - V // 2))
+    z[3, ::8] = 3 + rng.random(z[3, ::8].size)
+    z[4, ::64] = 3 + rng.random(z[4, ::64].size)
+    index, lp = run_top(torch.from_numpy(z).to(DEV), "f32", V, k)
+    want, wlp = R.top_logprobs(z.astype(np.float64), k)
+    assert np.array_equal(index, want)
+    within(lp, wlp, R.logprob_error(z, wlp))
+
+
+@pytest.mark.parametrize("V", [33, 1500, 66000])
+def test_excluded_classes(V):
+    """-inf: never chosen, log-probability -inf, gradient 0; rows where it leaves less than k classes, or none."""
+    rng = np.random.default_rng(V)
+    rows, k = 5, 20
+    z = rng.normal(0, 2, (rows, V)).astype(np.float32)
+    z[0, rng.random(V) < 0.5] = -np.inf
+    z[1, 7:] = -np.inf
+    z[2, :] = -np.inf
+    z[3, :-1] = -np.inf
+    buf, z64 = torch.from_numpy(z).to(DEV), z.astype(np.float64)
+    index, lp = run_top(buf, "f32", V, k)
+    want, wlp = R.top_logprobs(z64, k)
+    assert np.array_equal(index, want) and (index[2] == -1).all() and index[3, 1] == -1
+    within(lp, wlp, R.logprob_error(z64, wlp))
+    at = slots(rng, rows, V, k)
+    got, want = run_at(buf, "f32", V, at), R.logprobs_at(z64, at)
+    gone = want == -np.inf
+    assert gone.any() and np.array_equal(got == -np.inf, gone)
+    within(got[~gone], want[~gone], R.logprob_error(z64, want[~gone]))
+    sums = answers(rng, rows, k, 2)
+    at[0] = np.flatnonzero(z[0] > -np.inf)[:k] if (z[0] > -np.inf).sum() >= k else at[0, 0]
+    at[1, 0], at[1, 1:] = 3, -1
+    at[3] = V - 1
+    d = R.Distill(z64, at, sums, 2, 1.0)
+    loss, lse, grad = run_distill(buf, "f32", V, at, sums, 2, 1.0)
+    within(loss, d.loss, d.loss_error)
+    assert lse[2] == -np.inf and loss[2] == 0 and (grad[2] == 0).all()
+    within(grad, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+    assert (grad[0, z[0] == -np.inf] == 0).all()
+    back = run_distill(buf, "f32", V, at, sums, 2, 1.0, lse=lse)
+    d = R.Distill(z64, at, sums, 2, 1.0, lse=lse)
+    within(back, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+    # a teacher that wants an excluded class: infinite loss, a gradient nonetheless
+    at[1, 0] = V - 1
+    loss, lse, grad = run_distill(buf, "f32", V, at, sums, 2, 1.0)
+    assert loss[1] == np.inf and grad[1, V - 1] == -1 and np.isfinite(grad[1]).all()
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("V", [16, 900, 40000])
+def test_masks_of_the_lowest_value(dtype, V):
+    """Finite masks at the end of the type's range: no part in the sums, and a row of nothing else is uniform."""
+    rng = np.random.default_rng(V)
+    z = torch.from_numpy(rng.normal(0, 2, (3, V)).astype(np.float32)).to(TORCH[dtype])
+    low = torch.finfo(TORCH[dtype]).min
+    z[0, V // 2:] = low
+    z[1] = low
+    z[2, 1:] = low
+    z64, buf = z.double().numpy(), z.to(DEV)
+    at, sums = np.tile(np.array([0, 1, 5], np.int32), (3, 1)), answers(rng, 3, 3, 2)
+    d = R.Distill(z64, at, sums, 2, 1.0)
+    loss, lse, grad = run_distill(buf, dtype, V, at, sums, 2, 1.0)
+    within(grad, d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+    within(loss[1:2], d.loss[1:2], d.loss_error[1:2])
+    assert np.isfinite(lse).all()
+    index, lp = run_top(buf, dtype, V, 3)
+    want, wlp = R.top_logprobs(z64, 3)
+    assert np.array_equal(index, want)
+    within(lp[:2], wlp[:2], R.logprob_error(z64, wlp[:2]))
+
+
+@pytest.mark.parametrize("V", [40, 2000, 70001])
+def test_what_is_not_used_may_be_anything(V):
+    """NaN in padded rows, between rows, in empty slots; NaN and inf in one row stay in that row."""
+    rng = np.random.default_rng(V)
+    rows, k = 6, 11
+    buf, z = logits(rng, rows, V, 5, "f32")
+    index, sums = slots(rng, rows, V, k), answers(rng, rows, k, 3)
+    weight = np.ones(rows, np.float32)
+    weight[1] = 0
+    buf[1] = float("nan")
+    index[2] = -1
+    sums[2] = np.nan
+    buf[2, 3] = float("inf")
+    index[3, ::2], sums[3, ::2] = -1, np.nan
+    sums[4, 1:] = -np.inf                                          # one class has all of the teacher's mass
+    buf[5, V // 2] = float("nan")
+    z[[1, 2, 5]] = 0
+    d = R.Distill(z, index, sums, 3, 2.0, weight)
+    loss, lse, grad = run_distill(buf, "f32", V, index, sums, 3, 2.0, weight)
+    good = [0, 1, 2, 3, 4]
+    within(loss[good], d.loss[good], d.loss_error[good])
+    within(lse[good], d.lse[good], d.lse_error[good])
+    within(grad[good], d.grad[good], d.stored_error(HALF_STEP["f32"], LEAST["f32"])[good])
+    assert (grad[[1, 2]] == 0).all() and loss[1] == loss[2] == 0
+    assert np.isnan(loss[5]) and np.isnan(grad[5]).all()
+    top, lp = run_top(buf[:, :], "f32", V, 4)
+    want, _ = R.top_logprobs(buf[:, :V].double().cpu().numpy(), 4)
+    assert np.array_equal(top, want) and not (top[5] == V // 2).any()
+    assert (top[1] == -1).all() and (lp[1] == 0).all() and np.isnan(lp[5]).all()
+
+
+def test_rows_far_apart():
+    """Offsets beyond 2^32 elements, in the logits and in the gradient."""
+    rows, V, k, stride = 3, 1003, 6, (1 << 31) + 24
+    rng = np.random.default_rng(1)
+    z = torch.from_numpy(rng.normal(0, 3, (rows, V)).astype(np.float32)).half()
+    buf = torch.empty(rows * stride, dtype=torch.float16, device=DEV)
+    grad = torch.empty(rows * stride, dtype=torch.float16, device=DEV)
+    for r in range(rows):
+        buf[r * stride:r * stride + V] = z[r].to(DEV)
+        grad[r * stride + V] = GUARD
+    index, sums = slots(rng, rows, V, k), answers(rng, rows, k, 2)
+    d = R.Distill(z.double().numpy(), index, sums, 2, 1.0)
+    desc = B.make_logits(buf, B.F16, rows, V, row_stride=stride)
+    di, ds = dev(index), dev(sums)
+    t = B.make_teacher(di, ds, k, 2)
+    loss, lse = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+    s, n = scratch_for(desc, k)
+    for back in (False, True):
+        if back:
+            B.distill_backward(desc, t, lse, grad, stride)
+        else:
+            B.distill(desc, t, loss, lse, grad, stride, s, n)
+        torch.cuda.synchronize()
+        got = torch.stack([grad[r * stride:r * stride + V] for r in range(rows)]).double().cpu().numpy()
+        d = R.Distill(z.double().numpy(), index, sums, 2, 1.0, lse=lse.cpu().numpy() if back else None)
+        within(got, d.grad, d.stored_error(HALF_STEP["f16"], LEAST["f16"]))
+        assert all(grad[r * stride + V] == GUARD for r in range(rows))
+    top, lp = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV)
+    B.top_logprobs(desc, k, top, lp, s, n)
+    torch.cuda.synchronize()
+    assert np.array_equal(top.cpu().numpy(), R.top_logprobs(z.double().numpy(), k)[0])
+    B.logprobs_at(desc, di, k, lp, s, n)
+    torch.cuda.synchronize()
+    want = R.logprobs_at(z.double().numpy(), index)
+    within(lp.cpu().numpy(), want, R.logprob_error(z.double().numpy(), want))
+
+
+# ---- how it is called -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,V", [(300, 10), (64, 5000), (2, 131072), (700, 33000)])
+def test_the_same_call_gives_the_same_bits(rows, V):
+    rng = np.random.default_rng(rows)
+    buf, _ = logits(rng, rows, V, 0, "bf16")
+    index, sums = slots(rng, rows, V, 8, twice=True), answers(rng, rows, 8, 2)
+    first = run_distill(buf, "bf16", V, index, sums, 2, 1.0)
+    again = run_distill(buf, "bf16", V, index, sums, 2, 1.0)
+    assert all(np.array_equal(a, b) for a, b in zip(first, again))
+    assert all(np.array_equal(a, b) for a, b in zip(run_top(buf, "bf16", V, 8), run_top(buf, "bf16", V, 8)))
+
+
+@pytest.mark.parametrize("rows,V", [(256, 10), (3, 131072), (40, 5001)])
+def test_on_a_stream_and_in_a_replayed_graph(rows, V):
+    """One iteration's calls on a stream of their own and captured: every replay, with new inputs in place and eager work in
+    between, gives the bits of the eager calls.  Two graphs with a scratch each run at the same time."""
+    rng = np.random.default_rng(V)
+    k = 10
+
+    class Work:
+        def __init__(self):
+            self.buf = torch.empty((rows, V), dtype=torch.bfloat16, device=DEV)
+            self.sums = torch.empty((rows, k), device=DEV)
+            self.top = torch.empty((rows, k), dtype=torch.int32, device=DEV)
+            self.lp, self.at = torch.empty((rows, k), device=DEV), torch.empty((rows, k), device=DEV)
+            self.loss, self.lse = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+            self.grad, self.back = torch.empty_like(self.buf), torch.empty_like(self.buf)
+            self.z = describe(self.buf, "bf16", V)
+            self.t = B.make_teacher(self.top, self.sums, k, 3, 2.0)
+            self.s, self.n = scratch_for(self.z, k)
+
+        def fill(self):
+            self.buf.copy_(torch.from_numpy(rng.normal(0, 3, (rows, V)).astype(np.float32)))
+            self.sums.copy_(torch.from_numpy(answers(rng, rows, k, 3)))
+
+        def run(self, stream):
+            st = stream.cuda_stream
+            B.top_logprobs(self.z, k, self.top, self.lp, self.s, self.n, st)
+            B.logprobs_at(self.z, self.top, k, self.at, self.s, self.n, st)
+            B.distill(self.z, self.t, self.loss, self.lse, self.grad, V, self.s, self.n, st)
+            B.distill_backward(self.z, self.t, self.lse, self.back, V, st)
+
+        def results(self):
+            torch.cuda.synchronize()
+            return [x.clone() for x in (self.top, self.lp, self.at, self.loss, self.lse, self.grad, self.back)]
+
+    works, graphs, streams = [Work(), Work()], [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for w, side in zip(works, streams):
+        w.fill()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.stream(side):
+            w.run(side)
+            torch.cuda.synchronize()
+            with torch.cuda.graph(g, stream=side):
+                w.run(side)
+        graphs.append(g)
+    for _ in range(4):
+        want = []
+        for w, side in zip(works, streams):
+            w.fill()
+            torch.cuda.synchronize()
+            w.run(side)
+            want.append(w.results())
+            for x in (w.top, w.lp, w.at, w.loss, w.lse, w.grad, w.back):
+                x.zero_()
+        torch.cuda.synchronize()
+        for g, side in zip(graphs, streams):
+            with torch.cuda.stream(side):
+                g.replay()
+        for w, eager in zip(works, want):
+            for a, b in zip(w.results(), eager):
+                assert torch.equal(a, b)
