@@ -56,7 +56,24 @@ template <class F> d2mhe_status with_type(uint32_t dtype, F f)
     return hipGetLastError() == hipSuccess ? D2MHE_OK : D2MHE_ERR_HIP;
 }
 
-unsigned grid_of(uint32_t rows) { return rows < (1u << 20) ? rows : 1u << 20; }
+// f(T(), NT, NV): threads to a row and 16-byte words per thread, the fewest that hold a row; the longest keep a part of it.
+template <int NT, int NV> struct Shape {
+    static constexpr int THREADS = NT, WORDS = NV;
+};
+
+template <class F> d2mhe_status with_shape(const d2mhe_logits *z, F f)
+{
+    return with_type(z->dtype, [&](auto zero) {
+        const uint32_t words = (z->classes + Pack<decltype(zero)>::E - 1) / Pack<decltype(zero)>::E;
+        if (words <= 16) f(zero, Shape<16, 1>());
+        else if (words <= 128) f(zero, Shape<64, 2>());
+        else if (words <= 1024) f(zero, Shape<256, 4>());
+        else if (words <= 4096) f(zero, Shape<256, 16>());
+        else f(zero, Shape<1024, 16>());
+    });
+}
+
+template <int NT> unsigned grid_of(uint32_t rows) { return (rows + Group<NT>::ROWS - 1) / Group<NT>::ROWS; }
 
 }  // namespace
 
@@ -77,7 +94,7 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
     if (scratch_bytes < d2mhe_logits_scratch_bytes(z, k)) return D2MHE_ERR_WORKSPACE;
     if (z->rows == 0) return D2MHE_OK;
     return with_type(z->dtype, [&](auto zero) {
-        hipLaunchKernelGGL(k_top<decltype(zero)>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream, rows_of(z), k,
+        hipLaunchKernelGGL(k_top<decltype(zero)>, dim3(z->rows < (1u << 20) ? z->rows : 1u << 20), dim3(256), 0, (hipStream_t)stream, rows_of(z), k,
                            index, logprob);
     });
 }
@@ -90,9 +107,10 @@ d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint
     if (misaligned(z->logits) || misaligned(index) || misaligned(logprob) || misaligned(scratch)) return D2MHE_ERR_ALIGN;
     if (scratch_bytes < d2mhe_logits_scratch_bytes(z, k)) return D2MHE_ERR_WORKSPACE;
     if (z->rows == 0) return D2MHE_OK;
-    return with_type(z->dtype, [&](auto zero) {
-        hipLaunchKernelGGL(k_logprobs_at<decltype(zero)>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream,
-                           rows_of(z), index, k, logprob);
+    return with_shape(z, [&](auto zero, auto shape) {
+        constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
+        hipLaunchKernelGGL((k_logprobs_at<decltype(zero), NT, NV>), dim3(grid_of<NT>(z->rows)), dim3(Group<NT>::SIZE), 0,
+                           (hipStream_t)stream, rows_of(z), index, k, logprob);
     });
 }
 
@@ -108,10 +126,16 @@ d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, 
         if (d2mhe_status s = check_gradient(z, grad, grad_stride)) return s;
     if (scratch_bytes < d2mhe_logits_scratch_bytes(z, teacher->k)) return D2MHE_ERR_WORKSPACE;
     if (z->rows == 0) return D2MHE_OK;
-    return with_type(z->dtype, [&](auto zero) {
+    return with_shape(z, [&](auto zero, auto shape) {
         using T = decltype(zero);
-        hipLaunchKernelGGL(k_distill<T>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream, rows_of(z),
-                           answers_of(teacher), loss, lse, (T *)grad, grad_stride);
+        constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
+        const dim3 grid(grid_of<NT>(z->rows)), block(Group<NT>::SIZE);
+        if (grad)
+            hipLaunchKernelGGL((k_distill<T, NT, NV, true>), grid, block, 0, (hipStream_t)stream, rows_of(z),
+                               answers_of(teacher), loss, lse, (T *)grad, grad_stride);
+        else
+            hipLaunchKernelGGL((k_distill<T, NT, NV, false>), grid, block, 0, (hipStream_t)stream, rows_of(z),
+                               answers_of(teacher), loss, lse, (T *)nullptr, 0);
     });
 }
 
@@ -127,7 +151,7 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
     if (z->rows == 0) return D2MHE_OK;
     return with_type(z->dtype, [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL(k_distill_backward<T>, dim3(grid_of(z->rows)), dim3(256), 0, (hipStream_t)stream, rows_of(z),
+        hipLaunchKernelGGL(k_distill_backward<T>, dim3(z->rows), dim3(256), 0, (hipStream_t)stream, rows_of(z),
                            answers_of(teacher), lse, (T *)grad, grad_stride);
     });
 }

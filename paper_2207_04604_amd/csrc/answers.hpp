@@ -31,7 +31,126 @@ __device__ inline float to_float(__bf16 x) { return (float)x; }
 
 __device__ inline float neg_inf() { return -__builtin_inff(); }
 
-// ---- reductions over a workgroup of 256 ------------------------------------------------------------------
+// ---- 16 bytes of logits -----------------------------------------------------------------------------------
+
+typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
+// any alignment of an element: the machine takes 16-byte accesses at odd addresses
+typedef Word4 Word4Any __attribute__((aligned(2)));
+
+template <class T> struct Pack;                 // E elements in 16 bytes
+template <> struct Pack<float> {
+    static constexpr int E = 4;
+    static __device__ void open(Word4 w, float *x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(w[i]);
+    }
+    static __device__ Word4 close(const float *x)
+    {
+        Word4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+        return w;
+    }
+    static constexpr uint32_t NONE = 0xff800000u;                // -inf
+};
+template <> struct Pack<__bf16> {
+    static constexpr int E = 8;
+    static __device__ void open(Word4 w, float *x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ Word4 close(const float *x)
+    {
+        typedef __bf16 Two __attribute__((ext_vector_type(2)));
+        Word4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Two t = {(__bf16)x[2 * i], (__bf16)x[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, t);
+        }
+        return w;
+    }
+    static constexpr uint32_t NONE = 0xff80ff80u;
+};
+template <> struct Pack<_Float16> {
+    static constexpr int E = 8;
+    typedef _Float16 Two __attribute__((ext_vector_type(2)));
+    static __device__ void open(Word4 w, float *x)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t pair = w[i];          // a bit cast of w[i] itself reads element 0
+            const Two t = __builtin_bit_cast(Two, pair);
+            x[2 * i] = (float)t.x;
+            x[2 * i + 1] = (float)t.y;
+        }
+    }
+    static __device__ Word4 close(const float *x)
+    {
+        Word4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const Two t = {(_Float16)x[2 * i], (_Float16)x[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, t);
+        }
+        return w;
+    }
+    static constexpr uint32_t NONE = 0xfc00fc00u;
+};
+
+// fmaxf without the quieting of signalling NaNs that it costs on values that come straight from memory
+__device__ inline float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// ---- a row and the NT threads that work on it -------------------------------------------------------------
+
+// A workgroup has 256 threads or NT, whichever is more; groups of up to a wavefront never meet a barrier.
+template <int NT> struct Group {
+    static constexpr int SIZE = NT < 256 ? 256 : NT, ROWS = SIZE / NT, WAVES = NT < 64 ? 1 : NT / 64;
+    static constexpr int SLOTS = NT < (int)MAX_TOP ? (int)MAX_TOP / NT : 1;      // of a teacher, per thread
+
+    static __device__ uint32_t thread() { return threadIdx.x % NT; }
+    static __device__ uint32_t row_in_group() { return threadIdx.x / NT; }
+    static __device__ void sync()
+    {
+        if (NT > 64) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+    // sums (or maxima) of N values over the group, to every thread; buf: WAVES * N floats that nobody reads any more
+    template <class Op, int N> static __device__ void reduce(float *v, float *buf)
+    {
+#pragma unroll
+        for (int d = (NT < 64 ? NT : 64) / 2; d; d >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = Op::of(v[i], __shfl_xor(v[i], d));
+        if (NT > 64) {
+            if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i) buf[i * WAVES + (threadIdx.x >> 6)] = v[i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                float r = buf[i * WAVES];
+#pragma unroll
+                for (int k = 1; k < WAVES; ++k) r = Op::of(r, buf[i * WAVES + k]);
+                v[i] = r;
+            }
+        }
+    }
+};
 
 struct Max {
     static __device__ float of(float a, float b) { return fmaxf(a, b); }
@@ -40,52 +159,122 @@ struct Add {
     static __device__ float of(float a, float b) { return a + b; }
 };
 
-// every thread gets the result; `buf` is 4 floats of LDS that nothing else uses until the next barrier
-template <class Op> __device__ inline float block_reduce(float v, float *buf)
-{
-    for (int d = 32; d; d >>= 1) v = Op::of(v, __shfl_xor(v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-    __syncthreads();
-    return Op::of(Op::of(buf[0], buf[1]), Op::of(buf[2], buf[3]));
-}
+// The elements of a row: full 16-byte words from the first aligned address on, word c of the row with thread c % NT; the
+// words 0 .. NV * NT - 1 stay in registers, any others are read again by every pass.  What lies before and behind the
+// full words (at most 2 (E - 1) elements) goes one to a thread: `edge`, -inf where a thread has none.
+template <class T, int NT, int NV> struct Row {
+    using P = Pack<T>;
+    static constexpr int E = P::E;
+    const T *z;
+    const Word4 *words;
+    uint32_t head, n, at;           // elements before the words; words; position of the edge element (none: 0xffffffff)
+    float edge;
+    Word4 held[NV];
 
-// Maximum m and S = sum exp((z - m) / T) of a row.  (z - m) is rounded before the product with 1 / T, so that a row of the
-// type's lowest value gives S = classes and not inf - inf; a row of -inf gives S = 0.
-struct Stats {
-    float m, s;
+    __device__ void load(const T *row, uint32_t classes)
+    {
+        const uint32_t t = Group<NT>::thread();
+        z = row;
+        const uint32_t skip = (uint32_t)(-(uintptr_t)row & 15) / sizeof(T);
+        head = skip < classes ? skip : classes;
+        words = (const Word4 *)(row + head);
+        n = (classes - head) / E;
+        const uint32_t tail = (classes - head) % E;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            held[i] = Word4{P::NONE, P::NONE, P::NONE, P::NONE};
+            if ((uint32_t)i * NT < n) {
+                const uint32_t c = i * NT + t;
+                if (c < n) held[i] = words[c];
+            }
+        }
+        at = t < head ? t : t >= NT - tail ? classes - NT + t : 0xffffffffu;
+        edge = at != 0xffffffffu ? to_float(row[at]) : neg_inf();
+    }
+    // The words as they are, not as what an earlier pass made of them: the compiler would keep the opened elements of all
+    // words for the next pass, twice the registers of the words themselves.
+    __device__ Word4 fresh(int i)
+    {
+        asm("" : "+v"(held[i]));
+        return held[i];
+    }
+    // f(16 bytes): the words of this thread; words past the end hold -inf
+    template <class F> __device__ void each(F f)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((uint32_t)i * NT < n) f(fresh(i));
+        for (uint32_t c = NV * NT + Group<NT>::thread(); c < n; c += NT) f(words[c]);
+    }
+    // f(16 bytes, position of their first element): the words of this thread that the row has
+    template <class F> __device__ void each_at(F f)
+    {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if ((uint32_t)i * NT < n) {
+                const uint32_t c = i * NT + Group<NT>::thread();
+                if (c < n) f(fresh(i), head + c * E);
+            }
+        for (uint32_t c = NV * NT + Group<NT>::thread(); c < n; c += NT) f(words[c], head + c * E);
+    }
+    __device__ float max()
+    {
+        float m = edge;
+        each([&](Word4 w) {
+            float x[E];
+            P::open(w, x);
+#pragma unroll
+            for (int i = 0; i < E; i += 2) m = max3(m, x[i], x[i + 1]);
+        });
+        return m;
+    }
+    // sum exp2((x - base) * scale).  The difference is rounded before the product, so that a row of the type's lowest value
+    // gives 0 and not inf - inf.
+    __device__ float sum(float base, float scale)
+    {
+        float s = __builtin_amdgcn_exp2f((edge - base) * scale);
+        each([&](Word4 w) {
+            float x[E], part = 0;
+            P::open(w, x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) part += __builtin_amdgcn_exp2f((x[i] - base) * scale);
+            s += part;
+        });
+        return s;
+    }
 };
-
-template <class T> __device__ inline Stats row_stats(const T *z, uint32_t n, float scale, float *buf)
-{
-    float m = neg_inf();
-    for (uint32_t v = threadIdx.x; v < n; v += 256) m = fmaxf(m, to_float(z[v]));
-    m = block_reduce<Max>(m, buf);
-    const float base = m == neg_inf() ? 0.0f : m;
-    float s = 0;
-    for (uint32_t v = threadIdx.x; v < n; v += 256) s += __builtin_amdgcn_exp2f((to_float(z[v]) - base) * scale);
-    return {m, block_reduce<Add>(s, buf)};
-}
 
 // ---- log-probabilities at given classes ------------------------------------------------------------------
 
-template <class T>
-__global__ void __launch_bounds__(256) k_logprobs_at(Rows in, const int32_t *index, uint32_t k, float *out)
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(Group<NT>::SIZE) k_logprobs_at(Rows in, const int32_t *index, uint32_t k, float *out)
 {
-    __shared__ float buf[4];
-    for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
-        const T *z = (const T *)in.z + r * in.stride;
-        const Stats st = row_stats(z, in.classes, LOG2E, buf);
-        const float log_s = __logf(st.s);
-        for (uint32_t j = threadIdx.x; j < k; j += 256) {
-            const int32_t v = index[r * k + j];
-            float lp = 0;
-            if ((uint32_t)v < in.classes) {
-                const float x = to_float(z[v]);
-                lp = x == neg_inf() && st.s == st.s ? neg_inf() : (x - st.m) - log_s;
-            }
-            out[r * k + j] = lp;
-        }
+    using G = Group<NT>;
+    __shared__ float buf[2][G::WAVES];
+    const uint64_t r = (uint64_t)blockIdx.x * G::ROWS + G::row_in_group();
+    if (r >= in.rows) return;                       // NT > 64: the whole workgroup
+    int32_t at[G::SLOTS];
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i) {
+        const uint32_t j = i * NT + G::thread();
+        at[i] = j < k ? index[r * k + j] : -1;
+    }
+    Row<T, NT, NV> row;
+    row.load((const T *)in.z + r * in.stride, in.classes);
+    float x[G::SLOTS];
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i) x[i] = (uint32_t)at[i] < in.classes ? to_float(row.z[at[i]]) : 0.0f;
+    float m = row.max();
+    G::template reduce<Max, 1>(&m, buf[0]);
+    float s = row.sum(m == neg_inf() ? 0.0f : m, LOG2E);
+    G::template reduce<Add, 1>(&s, buf[1]);
+    const float log_s = __logf(s);
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i) {
+        const uint32_t j = i * NT + G::thread();
+        float lp = 0;
+        if ((uint32_t)at[i] < in.classes) lp = x[i] == neg_inf() && s == s ? neg_inf() : (x[i] - m) - log_s;
+        if (j < k) out[r * k + j] = lp;
     }
 }
 
@@ -118,9 +307,15 @@ __global__ void __launch_bounds__(256) k_top(Rows in, uint32_t k, int32_t *index
     __shared__ uint32_t need, done;
     for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
         const T *z = (const T *)in.z + r * in.stride;
-        const Stats st = row_stats(z, in.classes, LOG2E, buf);
-        const float log_s = __logf(st.s);
+        Row<T, 256, 1> row;
+        row.load(z, in.classes);
+        float m = row.max();
         __syncthreads();
+        Group<256>::reduce<Max, 1>(&m, buf);
+        __syncthreads();
+        float s = row.sum(m == neg_inf() ? 0.0f : m, LOG2E);
+        Group<256>::reduce<Add, 1>(&s, buf);
+        const float log_s = __logf(s);
         if (threadIdx.x == 0) {
             least = 0;
             need = k;
@@ -160,7 +355,7 @@ __global__ void __launch_bounds__(256) k_top(Rows in, uint32_t k, int32_t *index
                 uint32_t rank = 0;
                 for (uint32_t j = 0; j < n; ++j) rank += best[j] > key;
                 index[r * k + rank] = (int32_t)(0xffffffffu - (uint32_t)key);
-                out[r * k + rank] = (value_of((uint32_t)(key >> 32)) - st.m) - log_s;
+                out[r * k + rank] = (value_of((uint32_t)(key >> 32)) - m) - log_s;
             } else {
                 index[r * k + threadIdx.x] = -1;
                 out[r * k + threadIdx.x] = 0;
@@ -172,117 +367,168 @@ __global__ void __launch_bounds__(256) k_top(Rows in, uint32_t k, int32_t *index
 
 // ---- distillation ----------------------------------------------------------------------------------------
 
-// Slot j of a row belongs to thread j (k <= 256 = threads).
-struct Slot {
-    int32_t v;      // class, or -1: empty
-    float t, p;     // log p and p
+// The teacher's slots j of a row, slot j with thread j % NT: class (-1: empty) and answer s_j / T.
+template <int NT> struct Slots {
+    using G = Group<NT>;
+    int32_t v[G::SLOTS];
+    float t[G::SLOTS], u[G::SLOTS];
+
+    __device__ void load(const Answers &a, uint64_t r, uint32_t classes)
+    {
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i) {
+            const uint32_t j = i * NT + G::thread();
+            v[i] = -1;
+            t[i] = neg_inf();
+            if (j < a.k) {
+                const int32_t c = a.index[r * a.k + j];
+                const float s = a.sum[r * a.k + j];
+                if ((uint32_t)c < classes && s != neg_inf()) {
+                    v[i] = c;
+                    t[i] = s * a.inv_members * a.inv_t;
+                }
+            }
+        }
+    }
+    __device__ float max() const
+    {
+        float m = neg_inf();
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i) m = fmaxf(m, t[i]);
+        return m;
+    }
+    // u = exp(t - base), 0 in empty slots; returns their sum, and leaves classes and u in LDS
+    __device__ float weigh(float base, int32_t *vs, float *us)
+    {
+        float sum = 0;
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i) {
+            t[i] -= base;
+            u[i] = v[i] >= 0 ? __builtin_amdgcn_exp2f(t[i] * LOG2E) : 0.0f;
+            sum += u[i];
+            const uint32_t j = i * NT + G::thread();
+            if (j < MAX_TOP) {
+                vs[j] = v[i];
+                us[j] = u[i];
+            }
+        }
+        return sum;
+    }
+    // The u of all slots of a class are added up in slot order by each of them, so that a class given twice is stored twice
+    // with the same value.
+    __device__ float of_class(int32_t c, uint32_t k, const int32_t *vs, const float *us) const
+    {
+        float p = 0;
+        for (uint32_t j = 0; j < k; ++j) p += vs[j] == c ? us[j] : 0.0f;
+        return p;
+    }
 };
 
-// softmax over the filled slots; false: the row has none (the whole workgroup gets the same answer)
-__device__ inline bool teacher_slot(const Answers &a, uint64_t r, uint32_t classes, Slot &slot, float *buf)
+template <class T> __device__ inline void clear_row(T *out, uint32_t n, uint32_t t, uint32_t step)
 {
-    slot.v = -1;
-    slot.t = neg_inf();
-    if (threadIdx.x < a.k) {
-        const int32_t v = a.index[r * a.k + threadIdx.x];
-        const float t = a.sum[r * a.k + threadIdx.x];
-        if ((uint32_t)v < classes && t != neg_inf()) {
-            slot.v = v;
-            slot.t = t * a.inv_members * a.inv_t;
-        }
-    }
-    const bool some = __syncthreads_or(slot.v >= 0);
-    const float m = block_reduce<Max>(slot.t, buf);
-    slot.t -= m;
-    slot.p = slot.v >= 0 ? __builtin_amdgcn_exp2f(slot.t * LOG2E) : 0.0f;
-    const float s = block_reduce<Add>(slot.p, buf);
-    slot.t -= __logf(s);
-    slot.p /= s;
-    return some;
+    for (uint32_t v = t; v < n; v += step) out[v] = (T)0.0f;
 }
 
-// Gradient at the teacher's classes, over the dense part that the workgroup has stored: the p of all slots of a class are
-// added up in slot order by each of them, so that a class given twice is stored twice with the same value.
-template <class T>
-__device__ inline void store_slots(T *grad, const Slot &slot, float student, float g, uint32_t k, int32_t *vs, float *ps)
+// One pass over a row that stays in registers: its maximum m and S = sum exp((z - m) / T), then loss and gradient.  With
+// u_j = exp(t_j - t_max), U their sum, the three sums S, U and A = sum_j u_j (t_j - t_max - (z_j - m) / T) come out of one
+// reduction, and loss = A / U - log U + log S.
+template <class T, int NT, int NV, bool GRAD>
+__global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a, float *loss, float *lse, T *grad, uint64_t grad_stride)
 {
-    __syncthreads();
-    vs[threadIdx.x] = slot.v;
-    ps[threadIdx.x] = slot.p;
-    __syncthreads();
-    if (slot.v >= 0) {
-        float p = 0;
-        for (uint32_t j = 0; j < k; ++j) p += vs[j] == slot.v ? ps[j] : 0.0f;
-        grad[slot.v] = (T)((student - p) * g);
+    using G = Group<NT>;
+    using P = Pack<T>;
+    __shared__ float buf[5 * G::WAVES], us[G::ROWS][MAX_TOP];
+    __shared__ int32_t vs[G::ROWS][MAX_TOP];
+    const uint32_t group = G::row_in_group();
+    const uint64_t r = (uint64_t)blockIdx.x * G::ROWS + group;
+    if (r >= in.rows) return;                       // NT > 64: the whole workgroup
+    const float w = a.weight ? a.weight[r] : 1.0f, scale = a.inv_t * LOG2E;
+    T *out = GRAD ? grad + r * grad_stride : nullptr;
+    float m[2] = {neg_inf(), neg_inf()}, s[3] = {0, 0, 0};
+    Row<T, NT, NV> row;
+    Slots<NT> slots;
+    float x[G::SLOTS];
+    if (w != 0.0f) {
+        slots.load(a, r, in.classes);
+        row.load((const T *)in.z + r * in.stride, in.classes);
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i) x[i] = slots.v[i] >= 0 ? to_float(row.z[slots.v[i]]) : 0.0f;
+        m[1] = slots.max();
+        m[0] = row.max();
+        G::template reduce<Max, 2>(m, buf);
+        s[1] = slots.weigh(m[1], vs[group], us[group]);
+        const float base = m[0] == neg_inf() ? 0.0f : m[0];
+        s[0] = row.sum(base, scale);
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i) {
+            x[i] -= base;
+            if (slots.u[i] != 0.0f) s[2] += slots.u[i] * (slots.t[i] - x[i] * a.inv_t);
+        }
+        G::template reduce<Add, 3>(s, buf + 2 * G::WAVES);
     }
-}
-
-template <class T>
-__global__ void __launch_bounds__(256) k_distill(Rows in, Answers a, float *loss, float *lse, T *grad, uint64_t grad_stride)
-{
-    __shared__ float buf[4], ps[MAX_TOP];
-    __shared__ int32_t vs[MAX_TOP];
-    const float scale = a.inv_t * LOG2E;
-    for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
-        const T *z = (const T *)in.z + r * in.stride;
-        T *out = grad ? grad + r * grad_stride : nullptr;
-        const float w = a.weight ? a.weight[r] : 1.0f;
-        Slot slot;
-        bool live = w != 0.0f && teacher_slot(a, r, in.classes, slot, buf);
-        Stats st = {0, 0};
-        if (live) st = row_stats(z, in.classes, scale, buf);
-        const bool none = live && st.m == neg_inf() && st.s == 0.0f;     // all logits -inf
-        live = live && !none;
-        if (!live) {
-            if (threadIdx.x == 0) {
-                loss[r] = 0;
-                lse[r] = none ? neg_inf() : 0.0f;
-            }
-            if (out)
-                for (uint32_t v = threadIdx.x; v < in.classes; v += 256) out[v] = (T)0.0f;
-            continue;
+    // neither a filled slot nor a weight, or all logits -inf
+    const bool none = s[1] == 0.0f, excluded = !none && s[0] == 0.0f;
+    if (none || excluded) {
+        if (G::thread() == 0) {
+            loss[r] = 0;
+            lse[r] = none ? 0.0f : neg_inf();
         }
-        const float log_s = __logf(st.s), inv_s = 1.0f / st.s;
-        float x = 0, part = 0;
-        if (slot.v >= 0) {
-            x = to_float(z[slot.v]) - st.m;
-            part = slot.p > 0 || slot.p != slot.p ? slot.p * (slot.t - (x * a.inv_t - log_s)) : 0.0f;
-        }
-        part = block_reduce<Add>(part, buf);
-        if (threadIdx.x == 0) {
-            loss[r] = w * part;
-            lse[r] = st.m * a.inv_t + log_s;
-        }
-        if (!out) continue;
-        const float g = w * a.inv_t;
-        for (uint32_t v = threadIdx.x; v < in.classes; v += 256)
-            out[v] = (T)(__builtin_amdgcn_exp2f((to_float(z[v]) - st.m) * scale) * inv_s * g);
-        store_slots(out, slot, __builtin_amdgcn_exp2f(x * scale) * inv_s, g, a.k, vs, ps);
+        if (GRAD) clear_row(out, in.classes, G::thread(), NT);
+        return;
     }
+    const float log_s = __logf(s[0]);
+    if (G::thread() == 0) {
+        loss[r] = w * (s[2] / s[1] - __logf(s[1]) + log_s);
+        lse[r] = m[0] * a.inv_t + log_s;
+    }
+    if (!GRAD) return;
+    const float g = w * a.inv_t, gs = g / s[0], gu = g / s[1];
+    row.each_at([&](Word4 words, uint32_t v) {
+        float y[P::E];
+        P::open(words, y);
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) y[i] = __builtin_amdgcn_exp2f((y[i] - m[0]) * scale) * gs;
+        *(Word4Any *)(out + v) = P::close(y);
+    });
+    if (row.at != 0xffffffffu) out[row.at] = (T)(__builtin_amdgcn_exp2f((row.edge - m[0]) * scale) * gs);
+    // the teacher's classes, over the dense part
+    G::sync();
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i)
+        if (slots.v[i] >= 0)
+            out[slots.v[i]] = (T)(__builtin_amdgcn_exp2f(x[i] * scale) * gs - slots.of_class(slots.v[i], a.k, vs[group], us[group]) * gu);
 }
 
 template <class T>
 __global__ void __launch_bounds__(256) k_distill_backward(Rows in, Answers a, const float *lse, T *grad, uint64_t grad_stride)
 {
-    __shared__ float buf[4], ps[MAX_TOP];
+    using G = Group<256>;
+    __shared__ float buf[8], us[MAX_TOP];
     __shared__ int32_t vs[MAX_TOP];
-    for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
-        const T *z = (const T *)in.z + r * in.stride;
-        T *out = grad + r * grad_stride;
-        const float w = a.weight ? a.weight[r] : 1.0f, l = lse[r];
-        Slot slot;
-        const bool live = w != 0.0f && l != neg_inf() && teacher_slot(a, r, in.classes, slot, buf);
-        if (!live) {
-            for (uint32_t v = threadIdx.x; v < in.classes; v += 256) out[v] = (T)0.0f;
-            continue;
-        }
-        const float g = w * a.inv_t;
-        // z / T is not rounded before lse is taken off
-        auto student = [&](float x) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.inv_t, -l) * LOG2E); };
-        for (uint32_t v = threadIdx.x; v < in.classes; v += 256) out[v] = (T)(student(to_float(z[v])) * g);
-        const float p = slot.v >= 0 ? student(to_float(z[slot.v])) : 0.0f;
-        store_slots(out, slot, p, g, a.k, vs, ps);
+    const uint64_t r = blockIdx.x;
+    const T *z = (const T *)in.z + r * in.stride;
+    T *out = grad + r * grad_stride;
+    const float w = a.weight ? a.weight[r] : 1.0f, l = lse[r];
+    float m = neg_inf(), s = 0;
+    Slots<256> slots;
+    if (w != 0.0f && l != neg_inf()) {
+        slots.load(a, r, in.classes);
+        m = slots.max();
+        G::reduce<Max, 1>(&m, buf);
+        s = slots.weigh(m, vs, us);
+        G::reduce<Add, 1>(&s, buf + 4);
     }
+    if (s == 0.0f) {
+        clear_row(out, in.classes, threadIdx.x, 256);
+        return;
+    }
+    const float g = w * a.inv_t;
+    // z / T is not rounded before lse is taken off
+    auto student = [&](float x) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.inv_t, -l) * LOG2E); };
+    for (uint32_t v = threadIdx.x; v < in.classes; v += 256) out[v] = (T)(student(to_float(z[v])) * g);
+    __syncthreads();
+    if (slots.v[0] >= 0)
+        out[slots.v[0]] = (T)(student(to_float(z[slots.v[0]])) * g - slots.of_class(slots.v[0], a.k, vs, us) * (g / s));
 }
 
 }  // namespace answers
