@@ -40,7 +40,7 @@ d2mhe_status check_gradient(const d2mhe_logits *z, const void *grad, uint64_t st
     return D2MHE_OK;
 }
 
-Rows rows_of(const d2mhe_logits *z) { return {z->logits, z->row_stride, z->rows, z->classes}; }
+Rows rows_of(const d2mhe_logits *z) { return {z->logits, z->row_stride, 0, z->rows, z->classes}; }
 
 Answers answers_of(const d2mhe_teacher *t)
 {
@@ -56,15 +56,18 @@ template <class F> d2mhe_status with_type(uint32_t dtype, F f)
     return hipGetLastError() == hipSuccess ? D2MHE_OK : D2MHE_ERR_HIP;
 }
 
-// f(T(), NT, NV): threads to a row and 16-byte words per thread, the fewest that hold a row; the longest keep a part of it.
+template <class T> uint32_t words_of(const d2mhe_logits *z) { return (z->classes + Pack<T>::E - 1) / Pack<T>::E; }
+
+// threads to a row and 16-byte words per thread
 template <int NT, int NV> struct Shape {
     static constexpr int THREADS = NT, WORDS = NV;
 };
 
+// f(T(), Shape()): the fewest that hold a row; the longest rows keep a part of it
 template <class F> d2mhe_status with_shape(const d2mhe_logits *z, F f)
 {
     return with_type(z->dtype, [&](auto zero) {
-        const uint32_t words = (z->classes + Pack<decltype(zero)>::E - 1) / Pack<decltype(zero)>::E;
+        const uint32_t words = words_of<decltype(zero)>(z);
         if (words <= 16) f(zero, Shape<16, 1>());
         else if (words <= 128) f(zero, Shape<64, 2>());
         else if (words <= 1024) f(zero, Shape<256, 4>());
@@ -73,7 +76,17 @@ template <class F> d2mhe_status with_shape(const d2mhe_logits *z, F f)
     });
 }
 
-template <int NT> unsigned grid_of(uint32_t rows) { return (rows + Group<NT>::ROWS - 1) / Group<NT>::ROWS; }
+// launch(workgroups, rows from first on) until all rows are done: a launch has at most 2^20 workgroups
+template <int NT, class F> void each_launch(const d2mhe_logits *z, F launch)
+{
+    constexpr uint32_t PER = Group<NT>::ROWS;
+    Rows in = rows_of(z);
+    for (uint64_t first = 0; first < z->rows; first += (uint64_t)PER << 20) {
+        const uint64_t groups = (z->rows - first + PER - 1) / PER;
+        in.first = (uint32_t)first;
+        launch(dim3((unsigned)(groups < (1u << 20) ? groups : 1u << 20)), in);
+    }
+}
 
 }  // namespace
 
@@ -93,9 +106,23 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
     if (misaligned(z->logits) || misaligned(index) || misaligned(logprob) || misaligned(scratch)) return D2MHE_ERR_ALIGN;
     if (scratch_bytes < d2mhe_logits_scratch_bytes(z, k)) return D2MHE_ERR_WORKSPACE;
     if (z->rows == 0) return D2MHE_OK;
+    const auto run = [&](auto zero, auto shape) {
+        using T = decltype(zero);
+        constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
+        each_launch<NT>(z, [&](dim3 grid, Rows in) {
+            hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in, k, index, logprob);
+        });
+    };
+    // 16 threads have 16 maxima, which leaves few candidates to up to four slots; the 256 threads of a row of more than 1024
+    // words have room for a quarter of their maxima
     return with_type(z->dtype, [&](auto zero) {
-        hipLaunchKernelGGL(k_top<decltype(zero)>, dim3(z->rows < (1u << 20) ? z->rows : 1u << 20), dim3(256), 0, (hipStream_t)stream, rows_of(z), k,
-                           index, logprob);
+        const uint32_t words = words_of<decltype(zero)>(z);
+        if (words <= 16 && k <= 16) run(zero, Shape<16, 1>());
+        else if (words <= 128) run(zero, Shape<64, 2>());
+        else if (words <= 1024) run(zero, Shape<256, 4>());
+        else if (words <= 4096 && k <= 64) run(zero, Shape<256, 16>());
+        else if (words <= 4096) run(zero, Shape<1024, 4>());
+        else run(zero, Shape<1024, 16>());
     });
 }
 
@@ -109,8 +136,10 @@ d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint
     if (z->rows == 0) return D2MHE_OK;
     return with_shape(z, [&](auto zero, auto shape) {
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
-        hipLaunchKernelGGL((k_logprobs_at<decltype(zero), NT, NV>), dim3(grid_of<NT>(z->rows)), dim3(Group<NT>::SIZE), 0,
-                           (hipStream_t)stream, rows_of(z), index, k, logprob);
+        each_launch<NT>(z, [&](dim3 grid, Rows in) {
+            hipLaunchKernelGGL((k_logprobs_at<decltype(zero), NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in,
+                               index, k, logprob);
+        });
     });
 }
 
@@ -129,13 +158,14 @@ d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, 
     return with_shape(z, [&](auto zero, auto shape) {
         using T = decltype(zero);
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
-        const dim3 grid(grid_of<NT>(z->rows)), block(Group<NT>::SIZE);
-        if (grad)
-            hipLaunchKernelGGL((k_distill<T, NT, NV, true>), grid, block, 0, (hipStream_t)stream, rows_of(z),
-                               answers_of(teacher), loss, lse, (T *)grad, grad_stride);
-        else
-            hipLaunchKernelGGL((k_distill<T, NT, NV, false>), grid, block, 0, (hipStream_t)stream, rows_of(z),
-                               answers_of(teacher), loss, lse, (T *)nullptr, 0);
+        each_launch<NT>(z, [&](dim3 grid, Rows in) {
+            if (grad)
+                hipLaunchKernelGGL((k_distill<T, NT, NV, true>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in,
+                                   answers_of(teacher), loss, lse, (T *)grad, grad_stride);
+            else
+                hipLaunchKernelGGL((k_distill<T, NT, NV, false>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in,
+                                   answers_of(teacher), loss, lse, (T *)nullptr, 0);
+        });
     });
 }
 
@@ -151,8 +181,10 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
     if (z->rows == 0) return D2MHE_OK;
     return with_type(z->dtype, [&](auto zero) {
         using T = decltype(zero);
-        hipLaunchKernelGGL(k_distill_backward<T>, dim3(z->rows), dim3(256), 0, (hipStream_t)stream, rows_of(z),
-                           answers_of(teacher), lse, (T *)grad, grad_stride);
+        each_launch<256>(z, [&](dim3 grid, Rows in) {
+            hipLaunchKernelGGL(k_distill_backward<T>, grid, dim3(256), 0, (hipStream_t)stream, in, answers_of(teacher), lse,
+                               (T *)grad, grad_stride);
+        });
     });
 }
 

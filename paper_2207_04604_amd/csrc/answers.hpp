@@ -15,7 +15,7 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 struct Rows {
     const void *z;
     uint64_t stride;
-    uint32_t rows, classes;
+    uint32_t first, rows, classes;      // the launch's rows: first .. rows - 1
 };
 
 struct Answers {
@@ -217,6 +217,18 @@ template <class T, int NT, int NV> struct Row {
             }
         for (uint32_t c = NV * NT + Group<NT>::thread(); c < n; c += NT) f(words[c], head + c * E);
     }
+    // f(element, its position): all words once more from memory
+    template <class F> __device__ void elements_again(F f) const
+    {
+#pragma unroll 1
+        for (uint32_t c = Group<NT>::thread(); c < n; c += NT) {
+            float x[E];
+            P::open(words[c], x);
+#pragma unroll
+            for (int i = 0; i < E; ++i) f(x[i], head + c * E + i);
+        }
+        if (at != 0xffffffffu) f(edge, at);
+    }
     __device__ float max()
     {
         float m = edge;
@@ -251,7 +263,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_logprobs_at(Rows in, const 
 {
     using G = Group<NT>;
     __shared__ float buf[2][G::WAVES];
-    const uint64_t r = (uint64_t)blockIdx.x * G::ROWS + G::row_in_group();
+    const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + G::row_in_group();
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
     int32_t at[G::SLOTS];
 #pragma unroll
@@ -296,72 +308,193 @@ __device__ inline float value_of(uint32_t order)
 // order and position in one key: of equal values the lower class is the larger key; no two keys of a row are alike
 __device__ inline uint64_t key_of(float x, uint32_t v) { return (uint64_t)order_of(x) << 32 | (0xffffffffu - v); }
 
-// The k-th largest key digit by digit from the top: the counts of the next eight bits among the keys that agree with the
-// digits chosen so far.
-template <class T>
-__global__ void __launch_bounds__(256) k_top(Rows in, uint32_t k, int32_t *index, float *out)
+// The largest number t of the given leading bits with ballots for `count` of the keys at or above it, among the keys of all
+// threads of the group's wavefront (N keys to a thread); 0 if there are not as many keys above 0.
+template <int NT, int BITS, int N> __device__ inline uint32_t nth_largest(const uint32_t *keys, uint32_t count)
 {
-    __shared__ float buf[4];
-    __shared__ uint32_t count[256], found;
-    __shared__ uint64_t least, best[MAX_TOP];
+    uint32_t t = 0;
+#pragma unroll 1
+    for (uint32_t bit = 0x80000000u; bit >= (1u << (32 - BITS)) && bit; bit >>= 1) {
+        uint32_t above = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint64_t b = __ballot(keys[i] >= (t | bit));
+            above += NT >= 64 ? (uint32_t)__popcll(b) : (uint32_t)__popc((uint32_t)(b >> (threadIdx.x & 63 & ~(NT - 1))) & ((1u << (NT & 31)) - 1));
+        }
+        if (above >= count) t |= bit;
+    }
+    return t;
+}
+
+// bits of order_of that tell the values of a type apart
+template <class T> struct OrderBits { static constexpr int N = 32; };
+template <> struct OrderBits<__bf16> { static constexpr int N = 16; };
+template <> struct OrderBits<_Float16> { static constexpr int N = 19; };
+
+constexpr uint32_t CANDIDATES = 1024;
+
+// The k-th largest key digit by digit from the top: the counts of the next eight bits among the keys that agree with the
+// digits chosen so far. For rows with more candidates than LDS has room for, such as many equal values.
+template <int NT, class R> __device__ uint64_t least_by_digits(R &row, uint32_t k, uint32_t *count)
+{
+    __shared__ uint64_t least;
     __shared__ uint32_t need, done;
-    for (uint64_t r = blockIdx.x; r < in.rows; r += gridDim.x) {
-        const T *z = (const T *)in.z + r * in.stride;
-        Row<T, 256, 1> row;
-        row.load(z, in.classes);
-        float m = row.max();
+    if (threadIdx.x == 0) {
+        least = 0;
+        need = k;
+        done = 0;
+    }
+#pragma unroll 1
+    for (int shift = 56; shift >= 0; shift -= 8) {
+        if (threadIdx.x < 256) count[threadIdx.x] = 0;
         __syncthreads();
-        Group<256>::reduce<Max, 1>(&m, buf);
+        if (done) break;
+        const uint64_t prefix = least;
+        row.elements_again([&](float x, uint32_t v) {
+            const uint64_t key = key_of(x, v);
+            if ((key >> 32) && (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8))))
+                atomicAdd(&count[(key >> shift) & 255], 1u);
+        });
         __syncthreads();
-        float s = row.sum(m == neg_inf() ? 0.0f : m, LOG2E);
-        Group<256>::reduce<Add, 1>(&s, buf);
-        const float log_s = __logf(s);
         if (threadIdx.x == 0) {
-            least = 0;
-            need = k;
-            done = found = 0;
-        }
-        for (int shift = 56; shift >= 0; shift -= 8) {
-            count[threadIdx.x] = 0;
-            __syncthreads();
-            if (done) break;
-            const uint64_t prefix = least;
-            for (uint32_t v = threadIdx.x; v < in.classes; v += 256) {
-                const uint64_t key = key_of(to_float(z[v]), v);
-                if ((key >> 32) && (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8))))
-                    atomicAdd(&count[(key >> shift) & 255], 1u);
-            }
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                int d = 255;
-                uint32_t left = need;
-                while (d > 0 && count[d] < left) left -= count[d--];
-                least = prefix | (uint64_t)d << shift;
-                done = count[d] <= left;
-                need = left;
-            }
-            __syncthreads();
+            int d = 255;
+            uint32_t left = need;
+            while (d > 0 && count[d] < left) left -= count[d--];
+            least = prefix | (uint64_t)d << shift;
+            done = count[d] <= left;
+            need = left;
         }
         __syncthreads();
-        for (uint32_t v = threadIdx.x; v < in.classes; v += 256) {
-            const uint64_t key = key_of(to_float(z[v]), v);
-            if ((key >> 32) && key >= least) best[atomicAdd(&found, 1u)] = key;
+    }
+    __syncthreads();
+    return least;
+}
+
+// Two rounds over a row in registers.  The first gives the maximum of every thread; the `each`-th largest of a wavefront's
+// maxima, the least of them over the wavefronts, is a bound that at least k elements reach.  (Few words or many slots: the
+// bound comes from the elements themselves.)  The second collects what reaches it, usually little more than k, in LDS, where
+// every candidate counts the larger ones: that is its place.
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, int32_t *index, float *out)
+{
+    using G = Group<NT>;
+    using P = Pack<T>;
+    constexpr int BITS = OrderBits<T>::N, ROOM = NT < 64 ? 128 : CANDIDATES;
+    __shared__ float buf[2][G::WAVES];
+    __shared__ uint32_t bounds[G::WAVES], found[G::ROWS], words;
+    __shared__ __align__(16) uint64_t best[G::ROWS][ROOM];
+    const uint32_t group = G::row_in_group(), wave = NT > 64 ? threadIdx.x >> 6 : 0;
+    const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + group;
+    if (r >= in.rows) return;                       // NT > 64: the whole workgroup
+    Row<T, NT, NV> row;
+    row.load((const T *)in.z + r * in.stride, in.classes);
+    const float mine = row.max();
+    float m = mine;
+    if (G::thread() == 0) found[group] = 0;
+    if (threadIdx.x == 0) words = 0;
+    G::template reduce<Max, 1>(&m, buf[0]);
+    // wavefronts that have a word for every lane, or the only one
+    const uint32_t full = NT <= 64 ? 1 : row.n / 64 < G::WAVES ? row.n / 64 : G::WAVES, each = (k + full - 1) / full;
+    uint32_t bound;
+    if (NV <= 4 && 4 * k > (row.n < NT ? row.n : NT)) {
+        uint32_t keys[NV * P::E + 1];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[P::E];
+            P::open(row.fresh(i), x);
+#pragma unroll
+            for (int e = 0; e < P::E; ++e) keys[i * P::E + e] = order_of(x[e]);
         }
-        __syncthreads();
-        const uint32_t n = found;
-        if (threadIdx.x < k) {
-            if (threadIdx.x < n) {
-                const uint64_t key = best[threadIdx.x];
-                uint32_t rank = 0;
-                for (uint32_t j = 0; j < n; ++j) rank += best[j] > key;
-                index[r * k + rank] = (int32_t)(0xffffffffu - (uint32_t)key);
-                out[r * k + rank] = (value_of((uint32_t)(key >> 32)) - m) - log_s;
-            } else {
-                index[r * k + threadIdx.x] = -1;
-                out[r * k + threadIdx.x] = 0;
+        keys[NV * P::E] = order_of(row.edge);
+        bound = nth_largest<NT, BITS, NV * P::E + 1>(keys, each);
+    } else {
+        const uint32_t key = order_of(mine);
+        bound = nth_largest<NT, BITS, 1>(&key, each);
+    }
+    if (NT > 64) {
+        if ((threadIdx.x & 63) == 0) bounds[wave] = wave < full ? bound : 0xffffffffu;
+    }
+    float s = row.sum(m == neg_inf() ? 0.0f : m, LOG2E);
+    G::template reduce<Add, 1>(&s, buf[1]);
+    if (NT > 64) {
+        bound = bounds[0];
+        for (int i = 1; i < G::WAVES; ++i) bound = bounds[i] < bound ? bounds[i] : bound;
+    }
+    const float log_s = __logf(s);
+    // the least finite value leaves out -inf and NaN
+    const float least = bound ? value_of(bound) : -3.402823466e38f;
+    auto keep = [&](float x, uint32_t v) {
+        if (x >= least) {
+            const uint32_t i = atomicAdd(&found[group], 1u);
+            if (i < ROOM) best[group][i] = key_of(x, v);
+        }
+    };
+    if (row.at != 0xffffffffu) keep(row.edge, row.at);
+    auto reaches = [&](const float *x) {
+        float most = x[0];
+#pragma unroll
+        for (int i = 1; i + 1 < P::E; i += 2) most = max3(most, x[i], x[i + 1]);
+        return max3(most, x[P::E - 1], most) >= least;
+    };
+    if constexpr (NV <= 4) {
+        row.each_at([&](Word4 w, uint32_t v) {
+            float x[P::E];
+            P::open(w, x);
+            if (reaches(x))
+#pragma unroll
+                for (int i = 0; i < P::E; ++i) keep(x[i], v + i);
+        });
+    } else {
+        // whole words first, their elements then one to a thread: a body of all elements of all words would not fit the
+        // instruction cache
+        __shared__ Word4 word[CANDIDATES];
+        __shared__ uint32_t where[CANDIDATES];
+        row.each_at([&](Word4 w, uint32_t v) {
+            float x[P::E];
+            P::open(w, x);
+            if (reaches(x)) {
+                const uint32_t i = atomicAdd(&words, 1u);
+                if (i < CANDIDATES) {
+                    word[i] = w;
+                    where[i] = v;
+                }
             }
-        }
+        });
         __syncthreads();
+        const uint32_t all = words;
+        if (all <= CANDIDATES) {
+            for (uint32_t i = threadIdx.x; i < all * P::E; i += NT)
+                keep(to_float(((const T *)word)[i]), where[i / P::E] + i % P::E);
+        } else if (threadIdx.x == 0) {
+            found[0] = ROOM + 1;
+        }
+    }
+    G::sync();
+    uint32_t n = found[group];
+    if (NT > 64 && n > ROOM) {
+        __shared__ uint32_t count[256];
+        const uint64_t last = least_by_digits<NT>(row, k, count);
+        if (threadIdx.x == 0) found[0] = 0;
+        __syncthreads();
+        row.elements_again([&](float x, uint32_t v) {
+            const uint64_t key = key_of(x, v);
+            if ((key >> 32) && key >= last) best[0][atomicAdd(&found[0], 1u)] = key;
+        });
+        __syncthreads();
+        n = found[0];
+    }
+    for (uint32_t i = G::thread(); i < n; i += NT) {
+        const uint64_t key = best[group][i];
+        uint32_t place = 0;
+        for (uint32_t j = 0; j < n; ++j) place += best[group][j] > key;
+        if (place < k) {
+            index[r * k + place] = (int32_t)(0xffffffffu - (uint32_t)key);
+            out[r * k + place] = (value_of((uint32_t)(key >> 32)) - m) - log_s;
+        }
+    }
+    for (uint32_t i = n + G::thread(); i < k; i += NT) {
+        index[r * k + i] = -1;
+        out[r * k + i] = 0;
     }
 }
 
@@ -440,7 +573,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
     __shared__ float buf[5 * G::WAVES], us[G::ROWS][MAX_TOP];
     __shared__ int32_t vs[G::ROWS][MAX_TOP];
     const uint32_t group = G::row_in_group();
-    const uint64_t r = (uint64_t)blockIdx.x * G::ROWS + group;
+    const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + group;
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
     const float w = a.weight ? a.weight[r] : 1.0f, scale = a.inv_t * LOG2E;
     T *out = GRAD ? grad + r * grad_stride : nullptr;
@@ -505,7 +638,7 @@ __global__ void __launch_bounds__(256) k_distill_backward(Rows in, Answers a, co
     using G = Group<256>;
     __shared__ float buf[8], us[MAX_TOP];
     __shared__ int32_t vs[MAX_TOP];
-    const uint64_t r = blockIdx.x;
+    const uint64_t r = in.first + blockIdx.x;
     const T *z = (const T *)in.z + r * in.stride;
     T *out = grad + r * grad_stride;
     const float w = a.weight ? a.weight[r] : 1.0f, l = lse[r];
