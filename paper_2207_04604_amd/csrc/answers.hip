@@ -56,6 +56,8 @@ template <class F> d2mhe_status with_type(uint32_t dtype, F f)
     return hipGetLastError() == hipSuccess ? D2MHE_OK : D2MHE_ERR_HIP;
 }
 
+constexpr uint32_t SPLIT_ROWS = 192, SPLIT_GROUPS = 512, PART_WORDS = 1024;
+
 template <class T> uint32_t words_of(const d2mhe_logits *z) { return (z->classes + Pack<T>::E - 1) / Pack<T>::E; }
 
 // threads to a row and 16-byte words per thread
@@ -76,17 +78,35 @@ template <class F> d2mhe_status with_shape(const d2mhe_logits *z, F f)
     });
 }
 
+// How rows are cut into parts: not at all where there are rows enough to fill the chip.
+Parts parts_of(const d2mhe_logits *z, void *scratch)
+{
+    const uint32_t e = z->dtype == D2MHE_F32 ? 4 : 8, words = (z->classes + e - 1) / e;
+    Parts p = {1, words, (float2 *)scratch};
+    if (z->rows == 0 || z->rows >= SPLIT_ROWS || words <= PART_WORDS) return p;
+    uint32_t want = (SPLIT_GROUPS + z->rows - 1) / z->rows;
+    const uint32_t most = (words + PART_WORDS - 1) / PART_WORDS;
+    if (want > most) want = most;
+    if (want > 256) want = 256;
+    p.per = (words + want - 1) / want;
+    p.count = (words + p.per - 1) / p.per;
+    return p;
+}
+
 // launch(workgroups, rows from first on) until all rows are done: a launch has at most 2^20 workgroups
-template <int NT, class F> void each_launch(const d2mhe_logits *z, F launch)
+template <int NT, class F> void each_launch(const d2mhe_logits *z, uint32_t parts, F launch)
 {
     constexpr uint32_t PER = Group<NT>::ROWS;
+    const uint32_t most = parts < (1u << 20) ? (1u << 20) / parts : 1;          // rows (PER at a time) to a launch
     Rows in = rows_of(z);
-    for (uint64_t first = 0; first < z->rows; first += (uint64_t)PER << 20) {
+    for (uint64_t first = 0; first < z->rows; first += (uint64_t)PER * most) {
         const uint64_t groups = (z->rows - first + PER - 1) / PER;
         in.first = (uint32_t)first;
-        launch(dim3((unsigned)(groups < (1u << 20) ? groups : 1u << 20)), in);
+        launch(dim3((unsigned)(groups < most ? groups : most) * parts), in);
     }
 }
+
+template <int NT, class F> void each_launch(const d2mhe_logits *z, F launch) { each_launch<NT>(z, 1, launch); }
 
 }  // namespace
 
@@ -95,7 +115,8 @@ extern "C" {
 size_t d2mhe_logits_scratch_bytes(const d2mhe_logits *z, uint32_t k)
 {
     if (!z || !valid(z) || !valid_k(k)) return 0;
-    return 256;
+    const Parts p = parts_of(z, nullptr);
+    return p.count == 1 ? 256 : ((uint64_t)z->rows * p.count * sizeof(float2) + 255) / 256 * 256;
 }
 
 d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *index, float *logprob, void *scratch,
@@ -134,6 +155,15 @@ d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint
     if (misaligned(z->logits) || misaligned(index) || misaligned(logprob) || misaligned(scratch)) return D2MHE_ERR_ALIGN;
     if (scratch_bytes < d2mhe_logits_scratch_bytes(z, k)) return D2MHE_ERR_WORKSPACE;
     if (z->rows == 0) return D2MHE_OK;
+    const Parts parts = parts_of(z, scratch);
+    if (parts.count > 1)
+        return with_type(z->dtype, [&](auto zero) {
+            using T = decltype(zero);
+            hipLaunchKernelGGL((k_part_stats<T, 4>), dim3(z->rows * parts.count), dim3(256), 0, (hipStream_t)stream, rows_of(z),
+                               parts, LOG2E);
+            hipLaunchKernelGGL(k_part_logprobs<T>, dim3(z->rows), dim3(256), 0, (hipStream_t)stream, rows_of(z), parts, index, k,
+                               logprob);
+        });
     return with_shape(z, [&](auto zero, auto shape) {
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
         each_launch<NT>(z, [&](dim3 grid, Rows in) {
@@ -155,16 +185,30 @@ d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, 
         if (d2mhe_status s = check_gradient(z, grad, grad_stride)) return s;
     if (scratch_bytes < d2mhe_logits_scratch_bytes(z, teacher->k)) return D2MHE_ERR_WORKSPACE;
     if (z->rows == 0) return D2MHE_OK;
+    const Parts parts = parts_of(z, scratch);
+    const Answers a = answers_of(teacher);
+    if (parts.count > 1)
+        return with_type(z->dtype, [&](auto zero) {
+            using T = decltype(zero);
+            hipLaunchKernelGGL((k_part_stats<T, 4>), dim3(z->rows * parts.count), dim3(256), 0, (hipStream_t)stream, rows_of(z),
+                               parts, a.inv_t * LOG2E);
+            if (grad)
+                hipLaunchKernelGGL((k_gradient<T, 256, 4, true, true>), dim3(z->rows * parts.count), dim3(256), 0,
+                                   (hipStream_t)stream, rows_of(z), a, parts, loss, lse, (T *)grad, grad_stride);
+            else
+                hipLaunchKernelGGL((k_gradient<T, 256, 4, true, false>), dim3(z->rows), dim3(256), 0, (hipStream_t)stream,
+                                   rows_of(z), a, parts, loss, lse, (T *)nullptr, 0);
+        });
     return with_shape(z, [&](auto zero, auto shape) {
         using T = decltype(zero);
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
         each_launch<NT>(z, [&](dim3 grid, Rows in) {
             if (grad)
                 hipLaunchKernelGGL((k_distill<T, NT, NV, true>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in,
-                                   answers_of(teacher), loss, lse, (T *)grad, grad_stride);
+                                   a, loss, lse, (T *)grad, grad_stride);
             else
                 hipLaunchKernelGGL((k_distill<T, NT, NV, false>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in,
-                                   answers_of(teacher), loss, lse, (T *)nullptr, 0);
+                                   a, loss, lse, (T *)nullptr, 0);
         });
     });
 }
@@ -179,12 +223,20 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
         return D2MHE_ERR_ALIGN;
     if (d2mhe_status s = check_gradient(z, grad, grad_stride)) return s;
     if (z->rows == 0) return D2MHE_OK;
-    return with_type(z->dtype, [&](auto zero) {
+    const Answers a = answers_of(teacher);
+    const auto run = [&](auto zero, auto shape, Parts parts) {
         using T = decltype(zero);
-        each_launch<256>(z, [&](dim3 grid, Rows in) {
-            hipLaunchKernelGGL(k_distill_backward<T>, grid, dim3(256), 0, (hipStream_t)stream, in, answers_of(teacher), lse,
-                               (T *)grad, grad_stride);
+        constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
+        each_launch<NT>(z, parts.count, [&](dim3 grid, Rows in) {
+            hipLaunchKernelGGL((k_gradient<T, NT, NV, false, true>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in, a,
+                               parts, nullptr, const_cast<float *>(lse), (T *)grad, grad_stride);
         });
+    };
+    return with_type(z->dtype, [&](auto zero) {
+        const uint32_t words = words_of<decltype(zero)>(z);
+        if (words <= 16) run(zero, Shape<16, 1>(), Parts{1, words, nullptr});
+        else if (words <= 128) run(zero, Shape<64, 2>(), Parts{1, words, nullptr});
+        else run(zero, Shape<256, 4>(), Parts{(words + PART_WORDS - 1) / PART_WORDS, PART_WORDS, nullptr});
     });
 }
 

@@ -171,15 +171,21 @@ template <class T, int NT, int NV> struct Row {
     float edge;
     Word4 held[NV];
 
-    __device__ void load(const T *row, uint32_t classes)
+    // `first`, `count`: the words to take of the row, with the edges if the first is among them
+    __device__ void load(const T *row, uint32_t classes, uint32_t first = 0, uint32_t count = 0xffffffffu)
     {
         const uint32_t t = Group<NT>::thread();
         z = row;
         const uint32_t skip = (uint32_t)(-(uintptr_t)row & 15) / sizeof(T);
         head = skip < classes ? skip : classes;
-        words = (const Word4 *)(row + head);
         n = (classes - head) / E;
         const uint32_t tail = (classes - head) % E;
+        at = t < head ? t : t >= NT - tail ? classes - NT + t : 0xffffffffu;
+        if (first) at = 0xffffffffu;
+        head += first * E;
+        words = (const Word4 *)(row + head);
+        n = n > first ? n - first : 0;
+        n = n < count ? n : count;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             held[i] = Word4{P::NONE, P::NONE, P::NONE, P::NONE};
@@ -188,7 +194,6 @@ template <class T, int NT, int NV> struct Row {
                 if (c < n) held[i] = words[c];
             }
         }
-        at = t < head ? t : t >= NT - tail ? classes - NT + t : 0xffffffffu;
         edge = at != 0xffffffffu ? to_float(row[at]) : neg_inf();
     }
     // The words as they are, not as what an earlier pass made of them: the compiler would keep the opened elements of all
@@ -632,36 +637,151 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
             out[slots.v[i]] = (T)(__builtin_amdgcn_exp2f(x[i] * scale) * gs - slots.of_class(slots.v[i], a.k, vs[group], us[group]) * gu);
 }
 
-template <class T>
-__global__ void __launch_bounds__(256) k_distill_backward(Rows in, Answers a, const float *lse, T *grad, uint64_t grad_stride)
+// Rows of which there are few, or which no workgroup can hold, are cut into parts of `per` words, a workgroup of 256 to each.
+struct Parts {
+    uint32_t count, per;
+    float2 *stats;          // [rows][count]: maximum and sum of every part
+};
+
+template <class T, int NV> __global__ void __launch_bounds__(256) k_part_stats(Rows in, Parts parts, float scale)
 {
     using G = Group<256>;
-    __shared__ float buf[8], us[MAX_TOP];
-    __shared__ int32_t vs[MAX_TOP];
-    const uint64_t r = in.first + blockIdx.x;
-    const T *z = (const T *)in.z + r * in.stride;
-    T *out = grad + r * grad_stride;
-    const float w = a.weight ? a.weight[r] : 1.0f, l = lse[r];
-    float m = neg_inf(), s = 0;
-    Slots<256> slots;
-    if (w != 0.0f && l != neg_inf()) {
-        slots.load(a, r, in.classes);
-        m = slots.max();
-        G::reduce<Max, 1>(&m, buf);
-        s = slots.weigh(m, vs, us);
-        G::reduce<Add, 1>(&s, buf + 4);
+    __shared__ float buf[2][G::WAVES];
+    const uint64_t r = blockIdx.x / parts.count;
+    const uint32_t part = blockIdx.x % parts.count;
+    Row<T, 256, NV> row;
+    row.load((const T *)in.z + r * in.stride, in.classes, part * parts.per, parts.per);
+    float m = row.max();
+    G::reduce<Max, 1>(&m, buf[0]);
+    float s = row.sum(m == neg_inf() ? 0.0f : m, scale);
+    G::reduce<Add, 1>(&s, buf[1]);
+    if (threadIdx.x == 0) parts.stats[blockIdx.x] = make_float2(m, s);
+}
+
+// A thread's share of a row's parts, at most 256 parts: the maximum, then with the row's maximum its sum.
+struct Joined {
+    float m, s;
+    __device__ void load(const Parts &parts, uint64_t r)
+    {
+        m = neg_inf();
+        s = 0;
+        if (threadIdx.x < parts.count) {
+            const float2 v = parts.stats[r * parts.count + threadIdx.x];
+            m = v.x;
+            s = v.y;
+        }
     }
-    if (s == 0.0f) {
-        clear_row(out, in.classes, threadIdx.x, 256);
+    __device__ float sum(float base, float scale) const { return s == 0.0f ? 0.0f : s * __builtin_amdgcn_exp2f((m - base) * scale); }
+};
+
+// The gradient of a part of a row, or with NT < 256 of a whole one, from its statistics: the lse of an earlier call, or with
+// SPLIT the sums of its parts, where part 0 writes loss and lse as well.  Every part weighs the teacher's slots by itself and
+// stores those whose class it has.
+template <class T, int NT, int NV, bool SPLIT, bool GRAD>
+__global__ void __launch_bounds__(Group<NT>::SIZE)
+k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, uint64_t grad_stride)
+{
+    using G = Group<NT>;
+    using P = Pack<T>;
+    __shared__ float buf[5 * G::WAVES], us[G::ROWS][MAX_TOP];
+    __shared__ int32_t vs[G::ROWS][MAX_TOP];
+    const uint32_t group = G::row_in_group(), count = GRAD ? parts.count : 1;
+    const uint32_t part = NT < 256 ? 0 : blockIdx.x % count;
+    const uint64_t r = in.first + (NT < 256 ? (uint64_t)blockIdx.x * G::ROWS + group : blockIdx.x / count);
+    if (r >= in.rows) return;                       // NT > 64: the whole workgroup
+    const float w = a.weight ? a.weight[r] : 1.0f, scale = a.inv_t * LOG2E;
+    T *out = GRAD ? grad + r * grad_stride : nullptr;
+    const float l = SPLIT ? 0.0f : lse[r];
+    float m[2] = {neg_inf(), neg_inf()}, s[3] = {0, 0, 0};
+    Row<T, NT, NV> row;
+    Slots<NT> slots;
+    Joined joined;
+    float x[G::SLOTS];
+    row.n = 0;
+    const bool wanted = w != 0.0f && l != neg_inf();
+    if (wanted) {
+        slots.load(a, r, in.classes);
+        if (SPLIT) joined.load(parts, r);
+    }
+    if (GRAD) row.load((const T *)in.z + r * in.stride, in.classes, part * parts.per, parts.per);
+    if (wanted) {
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i)
+            x[i] = slots.v[i] >= 0 ? to_float(((const T *)in.z + r * in.stride)[slots.v[i]]) : 0.0f;
+        m[1] = slots.max();
+        if (SPLIT) {
+            m[0] = joined.m;
+            G::template reduce<Max, 2>(m, buf);
+        } else {
+            G::template reduce<Max, 1>(m + 1, buf);
+        }
+        s[1] = slots.weigh(m[1], vs[group], us[group]);
+        if (SPLIT) {
+            if (m[0] == neg_inf()) m[0] = 0;
+            s[0] = joined.sum(m[0], scale);
+#pragma unroll
+            for (int i = 0; i < G::SLOTS; ++i)
+                if (slots.u[i] != 0.0f) s[2] += slots.u[i] * (slots.t[i] - (x[i] - m[0]) * a.inv_t);
+            G::template reduce<Add, 3>(s, buf + 2 * G::WAVES);
+        } else {
+            G::template reduce<Add, 1>(s + 1, buf + 2 * G::WAVES);
+        }
+    }
+    const bool none = s[1] == 0.0f, excluded = SPLIT && !none && s[0] == 0.0f, zero = none || excluded;
+    if (SPLIT && part == 0 && G::thread() == 0) {
+        const float log_s = __logf(s[0]);
+        loss[r] = zero ? 0.0f : w * (s[2] / s[1] - __logf(s[1]) + log_s);
+        lse[r] = none ? 0.0f : excluded ? neg_inf() : m[0] * a.inv_t + log_s;
+    }
+    if (!GRAD) return;
+    // the row's share: what is taken off z / T, and the factor of exp
+    const float g = w * a.inv_t, gu = g / s[1], gs = zero ? 0.0f : SPLIT ? g / s[0] : g;
+    auto student = [&](float z) {
+        // z / T is not rounded before lse is taken off
+        return __builtin_amdgcn_exp2f(SPLIT ? (z - m[0]) * scale : __builtin_fmaf(z, a.inv_t, -l) * LOG2E) * gs;
+    };
+    if (zero) {
+        row.each_at([&](Word4, uint32_t v) { *(Word4Any *)(out + v) = Word4{0, 0, 0, 0}; });
+        if (row.at != 0xffffffffu) out[row.at] = (T)0.0f;
         return;
     }
-    const float g = w * a.inv_t;
-    // z / T is not rounded before lse is taken off
-    auto student = [&](float x) { return __builtin_amdgcn_exp2f(__builtin_fmaf(x, a.inv_t, -l) * LOG2E); };
-    for (uint32_t v = threadIdx.x; v < in.classes; v += 256) out[v] = (T)(student(to_float(z[v])) * g);
-    __syncthreads();
-    if (slots.v[0] >= 0)
-        out[slots.v[0]] = (T)(student(to_float(z[slots.v[0]])) * g - slots.of_class(slots.v[0], a.k, vs, us) * (g / s));
+    row.each_at([&](Word4 words, uint32_t v) {
+        float y[P::E];
+        P::open(words, y);
+#pragma unroll
+        for (int i = 0; i < P::E; ++i) y[i] = student(y[i]);
+        *(Word4Any *)(out + v) = P::close(y);
+    });
+    if (row.at != 0xffffffffu) out[row.at] = (T)student(row.edge);
+    G::sync();
+    // part 0 has the edges too: all classes before its words, and those behind the last part's
+    const uint32_t end = row.head + row.n * P::E, words_end = in.classes - (in.classes - row.head) % P::E;
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i) {
+        const uint32_t v = slots.v[i];
+        if (slots.v[i] >= 0 && ((v >= row.head && v < end) || (part == 0 && (v < row.head || v >= words_end))))
+            out[v] = (T)(student(x[i]) - slots.of_class(v, a.k, vs[group], us[group]) * gu);
+    }
+}
+
+// Log-probabilities of rows whose parts have been summed up.
+template <class T> __global__ void __launch_bounds__(256) k_part_logprobs(Rows in, Parts parts, const int32_t *index, uint32_t k, float *out)
+{
+    using G = Group<256>;
+    __shared__ float buf[2][G::WAVES];
+    const uint64_t r = blockIdx.x;
+    const T *z = (const T *)in.z + r * in.stride;
+    Joined joined;
+    joined.load(parts, r);
+    const uint32_t j = threadIdx.x;
+    const int32_t at = j < k ? index[r * k + j] : -1;
+    const bool filled = (uint32_t)at < in.classes;
+    const float x = filled ? to_float(z[at]) : 0.0f;
+    float m = joined.m;
+    G::reduce<Max, 1>(&m, buf[0]);
+    float s = joined.sum(m == neg_inf() ? 0.0f : m, LOG2E);
+    G::reduce<Add, 1>(&s, buf[1]);
+    if (j < k) out[r * k + j] = !filled ? 0.0f : x == neg_inf() && s == s ? neg_inf() : (x - m) - __logf(s);
 }
 
 }  // namespace answers
