@@ -65,15 +65,16 @@ template <int NT, int NV> struct Shape {
     static constexpr int THREADS = NT, WORDS = NV;
 };
 
-// f(T(), Shape()): the fewest that hold a row; the longest rows keep a part of it
-template <class F> d2mhe_status with_shape(const d2mhe_logits *z, F f)
+// f(T(), Shape()): the fewest that hold a row and its k slots; the longest rows keep a part of it
+template <class F> d2mhe_status with_shape(const d2mhe_logits *z, uint32_t k, F f)
 {
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
-        if (words <= 16) f(zero, Shape<16, 1>());
+        if (words <= 16 && k <= Group<16>::TOP) f(zero, Shape<16, 1>());
         else if (words <= 128) f(zero, Shape<64, 2>());
         else if (words <= 1024) f(zero, Shape<256, 4>());
         else if (words <= 4096) f(zero, Shape<256, 16>());
+        else if (words <= 8192) f(zero, Shape<512, 16>());
         else f(zero, Shape<1024, 16>());
     });
 }
@@ -164,7 +165,7 @@ d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint
             hipLaunchKernelGGL(k_part_logprobs<T>, dim3(z->rows), dim3(256), 0, (hipStream_t)stream, rows_of(z), parts, index, k,
                                logprob);
         });
-    return with_shape(z, [&](auto zero, auto shape) {
+    return with_shape(z, k, [&](auto zero, auto shape) {
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
         each_launch<NT>(z, [&](dim3 grid, Rows in) {
             hipLaunchKernelGGL((k_logprobs_at<decltype(zero), NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in,
@@ -199,7 +200,7 @@ d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, 
                 hipLaunchKernelGGL((k_gradient<T, 256, 4, true, false>), dim3(z->rows), dim3(256), 0, (hipStream_t)stream,
                                    rows_of(z), a, parts, loss, lse, (T *)nullptr, 0);
         });
-    return with_shape(z, [&](auto zero, auto shape) {
+    return with_shape(z, teacher->k, [&](auto zero, auto shape) {
         using T = decltype(zero);
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
         each_launch<NT>(z, [&](dim3 grid, Rows in) {
@@ -234,7 +235,7 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
     };
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
-        if (words <= 16) run(zero, Shape<16, 1>(), Parts{1, words, nullptr});
+        if (words <= 16 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 1>(), Parts{1, words, nullptr});
         else if (words <= 128) run(zero, Shape<64, 2>(), Parts{1, words, nullptr});
         else run(zero, Shape<256, 4>(), Parts{(words + PART_WORDS - 1) / PART_WORDS, PART_WORDS, nullptr});
     });

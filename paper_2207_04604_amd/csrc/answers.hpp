@@ -116,7 +116,7 @@ __device__ inline float max3(float a, float b, float c)
 // A workgroup has 256 threads or NT, whichever is more; groups of up to a wavefront never meet a barrier.
 template <int NT> struct Group {
     static constexpr int SIZE = NT < 256 ? 256 : NT, ROWS = SIZE / NT, WAVES = NT < 64 ? 1 : NT / 64;
-    static constexpr int SLOTS = NT < (int)MAX_TOP ? (int)MAX_TOP / NT : 1;      // of a teacher, per thread
+    static constexpr int TOP = NT < 64 ? 64 : MAX_TOP, SLOTS = NT < TOP ? TOP / NT : 1;     // slots of a row, of a thread
 
     static __device__ uint32_t thread() { return threadIdx.x % NT; }
     static __device__ uint32_t row_in_group() { return threadIdx.x / NT; }
@@ -505,6 +505,22 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
 
 // ---- distillation ----------------------------------------------------------------------------------------
 
+// What a row's threads have to know of each other's slots.
+template <int NT> struct Taught {
+    using G = Group<NT>;
+    static constexpr uint32_t PLACES = 2 * G::TOP;
+    int32_t v[G::ROWS][G::TOP];
+    float u[G::ROWS][G::TOP];
+    int32_t place[G::ROWS][PLACES];
+    uint32_t twice[G::ROWS];
+
+    __device__ void clear(uint32_t group)
+    {
+        for (uint32_t i = G::thread(); i < PLACES; i += NT) place[group][i] = -1;
+        if (G::thread() == 0) twice[group] = 0;
+    }
+};
+
 // The teacher's slots j of a row, slot j with thread j % NT: class (-1: empty) and answer s_j / T.
 template <int NT> struct Slots {
     using G = Group<NT>;
@@ -535,29 +551,45 @@ template <int NT> struct Slots {
         for (int i = 0; i < G::SLOTS; ++i) m = fmaxf(m, t[i]);
         return m;
     }
-    // u = exp(t - base), 0 in empty slots; returns their sum, and leaves classes and u in LDS
-    __device__ float weigh(float base, int32_t *vs, float *us)
+    // u = exp(t - base), 0 in empty slots; returns their sum.  Leaves classes and u in LDS, and there whether a class comes
+    // twice: of two slots of a class one finds the other in a table of twice as many places as slots.
+    __device__ float weigh(float base, uint32_t k, Taught<NT> &lds, uint32_t group)
     {
         float sum = 0;
+        if (NT <= 64) G::sync();                    // others have met a barrier since the table was cleared
 #pragma unroll
         for (int i = 0; i < G::SLOTS; ++i) {
+            u[i] = 0;
+            if (v[i] < 0) continue;
             t[i] -= base;
-            u[i] = v[i] >= 0 ? __builtin_amdgcn_exp2f(t[i] * LOG2E) : 0.0f;
+            u[i] = __builtin_amdgcn_exp2f(t[i] * LOG2E);
             sum += u[i];
+            constexpr uint32_t LAST = Taught<NT>::PLACES - 1;
+            uint32_t h = ((uint32_t)v[i] * 0x9e3779b1u) >> 16 & LAST;
+            while (true) {                          // ends: half of the places stay free
+                const int32_t there = atomicCAS(&lds.place[group][h], -1, v[i]);
+                if (there == v[i]) lds.twice[group] = 1;
+                if (there < 0 || there == v[i]) break;
+                h = (h + 1) & LAST;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i) {
             const uint32_t j = i * NT + G::thread();
-            if (j < MAX_TOP) {
-                vs[j] = v[i];
-                us[j] = u[i];
+            if (j < k) {
+                lds.v[group][j] = v[i];
+                lds.u[group][j] = u[i];
             }
         }
         return sum;
     }
-    // The u of all slots of a class are added up in slot order by each of them, so that a class given twice is stored twice
-    // with the same value.
-    __device__ float of_class(int32_t c, uint32_t k, const int32_t *vs, const float *us) const
+    // The u of slot i, or where classes come twice those of all slots of its class, added up in slot order: each of them is
+    // stored with the same value.
+    __device__ float of_class(int i, uint32_t k, const Taught<NT> &lds, uint32_t group) const
     {
+        if (!lds.twice[group]) return u[i];
         float p = 0;
-        for (uint32_t j = 0; j < k; ++j) p += vs[j] == c ? us[j] : 0.0f;
+        for (uint32_t j = 0; j < k; ++j) p += lds.v[group][j] == v[i] ? lds.u[group][j] : 0.0f;
         return p;
     }
 };
@@ -575,8 +607,8 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
 {
     using G = Group<NT>;
     using P = Pack<T>;
-    __shared__ float buf[5 * G::WAVES], us[G::ROWS][MAX_TOP];
-    __shared__ int32_t vs[G::ROWS][MAX_TOP];
+    __shared__ float buf[5 * G::WAVES];
+    __shared__ Taught<NT> taught;
     const uint32_t group = G::row_in_group();
     const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + group;
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
@@ -586,6 +618,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
     Row<T, NT, NV> row;
     Slots<NT> slots;
     float x[G::SLOTS];
+    taught.clear(group);
     if (w != 0.0f) {
         slots.load(a, r, in.classes);
         row.load((const T *)in.z + r * in.stride, in.classes);
@@ -594,7 +627,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
         m[1] = slots.max();
         m[0] = row.max();
         G::template reduce<Max, 2>(m, buf);
-        s[1] = slots.weigh(m[1], vs[group], us[group]);
+        s[1] = slots.weigh(m[1], a.k, taught, group);
         const float base = m[0] == neg_inf() ? 0.0f : m[0];
         s[0] = row.sum(base, scale);
 #pragma unroll
@@ -634,7 +667,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
 #pragma unroll
     for (int i = 0; i < G::SLOTS; ++i)
         if (slots.v[i] >= 0)
-            out[slots.v[i]] = (T)(__builtin_amdgcn_exp2f(x[i] * scale) * gs - slots.of_class(slots.v[i], a.k, vs[group], us[group]) * gu);
+            out[slots.v[i]] = (T)(__builtin_amdgcn_exp2f(x[i] * scale) * gs - slots.of_class(i, a.k, taught, group) * gu);
 }
 
 // Rows of which there are few, or which no workgroup can hold, are cut into parts of `per` words, a workgroup of 256 to each.
@@ -683,8 +716,8 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
 {
     using G = Group<NT>;
     using P = Pack<T>;
-    __shared__ float buf[5 * G::WAVES], us[G::ROWS][MAX_TOP];
-    __shared__ int32_t vs[G::ROWS][MAX_TOP];
+    __shared__ float buf[5 * G::WAVES];
+    __shared__ Taught<NT> taught;
     const uint32_t group = G::row_in_group(), count = GRAD ? parts.count : 1;
     const uint32_t part = NT < 256 ? 0 : blockIdx.x % count;
     const uint64_t r = in.first + (NT < 256 ? (uint64_t)blockIdx.x * G::ROWS + group : blockIdx.x / count);
@@ -697,7 +730,7 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     Slots<NT> slots;
     Joined joined;
     float x[G::SLOTS];
-    row.n = 0;
+    taught.clear(group);
     const bool wanted = w != 0.0f && l != neg_inf();
     if (wanted) {
         slots.load(a, r, in.classes);
@@ -715,7 +748,7 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
         } else {
             G::template reduce<Max, 1>(m + 1, buf);
         }
-        s[1] = slots.weigh(m[1], vs[group], us[group]);
+        s[1] = slots.weigh(m[1], a.k, taught, group);
         if (SPLIT) {
             if (m[0] == neg_inf()) m[0] = 0;
             s[0] = joined.sum(m[0], scale);
@@ -760,7 +793,7 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     for (int i = 0; i < G::SLOTS; ++i) {
         const uint32_t v = slots.v[i];
         if (slots.v[i] >= 0 && ((v >= row.head && v < end) || (part == 0 && (v < row.head || v >= words_end))))
-            out[v] = (T)(student(x[i]) - slots.of_class(v, a.k, vs[group], us[group]) * gu);
+            out[v] = (T)(student(x[i]) - slots.of_class(i, a.k, taught, group) * gu);
     }
 }
 
