@@ -83,7 +83,7 @@ template <class F> d2mhe_status with_shape(const d2mhe_logits *z, uint32_t k, F 
 Parts parts_of(const d2mhe_logits *z, void *scratch)
 {
     const uint32_t e = z->dtype == D2MHE_F32 ? 4 : 8, words = (z->classes + e - 1) / e;
-    Parts p = {1, words, (float2 *)scratch};
+    Parts p = {1, words, (Stats *)scratch};
     if (z->rows == 0 || z->rows >= SPLIT_ROWS || words <= PART_WORDS) return p;
     uint32_t want = (SPLIT_GROUPS + z->rows - 1) / z->rows;
     const uint32_t most = (words + PART_WORDS - 1) / PART_WORDS;
@@ -117,7 +117,7 @@ size_t d2mhe_logits_scratch_bytes(const d2mhe_logits *z, uint32_t k)
 {
     if (!z || !valid(z) || !valid_k(k)) return 0;
     const Parts p = parts_of(z, nullptr);
-    return p.count == 1 ? 256 : ((uint64_t)z->rows * p.count * sizeof(float2) + 255) / 256 * 256;
+    return p.count == 1 ? 256 : ((uint64_t)z->rows * p.count * sizeof(Stats) + 255) / 256 * 256;
 }
 
 d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *index, float *logprob, void *scratch,

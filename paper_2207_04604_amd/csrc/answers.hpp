@@ -10,7 +10,7 @@ namespace d2 {
 namespace answers {
 
 constexpr uint32_t MAX_TOP = D2MHE_MAX_TOP;
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+constexpr float LOG2E = 1.44269504088896340736f;
 
 struct Rows {
     const void *z;
@@ -113,13 +113,66 @@ __device__ inline float max3(float a, float b, float c)
 
 // ---- a row and the NT threads that work on it -------------------------------------------------------------
 
+struct Max {
+    static __device__ float of(float a, float b) { return fmaxf(a, b); }
+};
+struct Add {
+    static __device__ float of(float a, float b) { return a + b; }
+    static __device__ uint32_t of(uint32_t a, uint32_t b) { return a + b; }
+};
+
+template <int ROR, class V> __device__ inline V rotated(V v)            // lane l of 16: what lane l - ROR holds
+{
+    const int i = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(i, i, 0x120 + ROR, 0xf, 0xf, false));
+}
+
+// Op over the W neighbouring lanes of a lane, in all of them and to the same bits: rotations within 16 lanes, then exchanges
+// of halves (register moves, where a shuffle goes through LDS).
+template <class Op, int W, class V> __device__ inline V across(V v)
+{
+    if (W >= 2) v = Op::of(v, rotated<W >= 16 ? 8 : W >= 8 ? 4 : W >= 4 ? 2 : 1>(v));
+    if (W >= 4) v = Op::of(v, rotated<W >= 16 ? 4 : W >= 8 ? 2 : 1>(v));
+    if (W >= 8) v = Op::of(v, rotated<W >= 16 ? 2 : 1>(v));
+    if (W >= 16) v = Op::of(v, rotated<1>(v));
+    if (W >= 32) {
+        const uint32_t i = __builtin_bit_cast(uint32_t, v);
+        const auto halves = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+        const uint32_t x = halves[0], y = halves[1];
+        v = Op::of(__builtin_bit_cast(V, x), __builtin_bit_cast(V, y));
+    }
+    if (W >= 64) {
+        const uint32_t i = __builtin_bit_cast(uint32_t, v);
+        const auto halves = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+        const uint32_t x = halves[0], y = halves[1];
+        v = Op::of(__builtin_bit_cast(V, x), __builtin_bit_cast(V, y));
+    }
+    return v;
+}
+
+// Maximum m and s = sum exp2((x - m) * scale) of some elements.  (x - m) is rounded before the product, so that elements of
+// the type's lowest value give their number and not inf - inf; elements of -inf give m = -inf, s = 0.
+struct Stats {
+    float m, s;
+
+    // s as seen from another maximum
+    __device__ float at(float top, float scale) const { return s == 0.0f ? 0.0f : s * __builtin_amdgcn_exp2f((m - top) * scale); }
+    // of the W neighbouring lanes
+    template <int W> __device__ Stats together(float scale) const
+    {
+        const float top = across<Max, W>(m);
+        return {top, across<Add, W>(at(top, scale))};
+    }
+};
+
 // A workgroup has 256 threads or NT, whichever is more; groups of up to a wavefront never meet a barrier.
 template <int NT> struct Group {
-    static constexpr int SIZE = NT < 256 ? 256 : NT, ROWS = SIZE / NT, WAVES = NT < 64 ? 1 : NT / 64;
+    static constexpr int SIZE = NT < 256 ? 256 : NT, ROWS = SIZE / NT, WAVES = NT < 64 ? 1 : NT / 64, LANES = NT < 64 ? NT : 64;
     static constexpr int TOP = NT < 64 ? 64 : MAX_TOP, SLOTS = NT < TOP ? TOP / NT : 1;     // slots of a row, of a thread
 
     static __device__ uint32_t thread() { return threadIdx.x % NT; }
     static __device__ uint32_t row_in_group() { return threadIdx.x / NT; }
+    static __device__ uint32_t wave() { return NT > 64 ? threadIdx.x >> 6 : 0; }
     static __device__ void sync()
     {
         if (NT > 64) {
@@ -129,41 +182,26 @@ template <int NT> struct Group {
             __builtin_amdgcn_wave_barrier();
         }
     }
-    // sums (or maxima) of N values over the group, to every thread; buf: WAVES * N floats that nobody reads any more
-    template <class Op, int N> static __device__ void reduce(float *v, float *buf)
+    // Statistics of a wavefront's lanes to those of the group, over a barrier between the two calls.
+    static __device__ void put(Stats v, Stats *buf)
     {
-#pragma unroll
-        for (int d = (NT < 64 ? NT : 64) / 2; d; d >>= 1)
-#pragma unroll
-            for (int i = 0; i < N; ++i) v[i] = Op::of(v[i], __shfl_xor(v[i], d));
-        if (NT > 64) {
-            if ((threadIdx.x & 63) == 0)
-#pragma unroll
-                for (int i = 0; i < N; ++i) buf[i * WAVES + (threadIdx.x >> 6)] = v[i];
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                float r = buf[i * WAVES];
-#pragma unroll
-                for (int k = 1; k < WAVES; ++k) r = Op::of(r, buf[i * WAVES + k]);
-                v[i] = r;
-            }
-        }
+        if (NT > 64 && (threadIdx.x & 63) == 0) buf[wave()] = v;
+    }
+    static __device__ Stats get(Stats v, const Stats *buf, float scale)
+    {
+        if (NT <= 64) return v;
+        return buf[threadIdx.x % WAVES].template together<WAVES>(scale);
     }
 };
 
-struct Max {
-    static __device__ float of(float a, float b) { return fmaxf(a, b); }
-};
-struct Add {
-    static __device__ float of(float a, float b) { return a + b; }
-};
+constexpr float FAR = 4194304.0f;       // from here on x * scale has no bits to spare next to the whole numbers
 
 // The elements of a row: full 16-byte words from the first aligned address on, word c of the row with thread c % NT; the
 // words 0 .. NV * NT - 1 stay in registers, any others are read again by every pass.  What lies before and behind the
 // full words (at most 2 (E - 1) elements) goes one to a thread: `edge`, -inf where a thread has none.
 template <class T, int NT, int NV> struct Row {
     using P = Pack<T>;
+    using G = Group<NT>;
     static constexpr int E = P::E;
     const T *z;
     const Word4 *words;
@@ -172,9 +210,9 @@ template <class T, int NT, int NV> struct Row {
     Word4 held[NV];
 
     // `first`, `count`: the words to take of the row, with the edges if the first is among them
-    __device__ void load(const T *row, uint32_t classes, uint32_t first = 0, uint32_t count = 0xffffffffu)
+    __device__ void place(const T *row, uint32_t classes, uint32_t first = 0, uint32_t count = 0xffffffffu)
     {
-        const uint32_t t = Group<NT>::thread();
+        const uint32_t t = G::thread();
         z = row;
         const uint32_t skip = (uint32_t)(-(uintptr_t)row & 15) / sizeof(T);
         head = skip < classes ? skip : classes;
@@ -186,6 +224,10 @@ template <class T, int NT, int NV> struct Row {
         words = (const Word4 *)(row + head);
         n = n > first ? n - first : 0;
         n = n < count ? n : count;
+    }
+    __device__ void load()
+    {
+        const uint32_t t = G::thread();
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             held[i] = Word4{P::NONE, P::NONE, P::NONE, P::NONE};
@@ -194,7 +236,7 @@ template <class T, int NT, int NV> struct Row {
                 if (c < n) held[i] = words[c];
             }
         }
-        edge = at != 0xffffffffu ? to_float(row[at]) : neg_inf();
+        edge = at != 0xffffffffu ? to_float(z[at]) : neg_inf();
     }
     // The words as they are, not as what an earlier pass made of them: the compiler would keep the opened elements of all
     // words for the next pass, twice the registers of the words themselves.
@@ -209,7 +251,7 @@ template <class T, int NT, int NV> struct Row {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if ((uint32_t)i * NT < n) f(fresh(i));
-        for (uint32_t c = NV * NT + Group<NT>::thread(); c < n; c += NT) f(words[c]);
+        for (uint32_t c = NV * NT + G::thread(); c < n; c += NT) f(words[c]);
     }
     // f(16 bytes, position of their first element): the words of this thread that the row has
     template <class F> __device__ void each_at(F f)
@@ -217,47 +259,109 @@ template <class T, int NT, int NV> struct Row {
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             if ((uint32_t)i * NT < n) {
-                const uint32_t c = i * NT + Group<NT>::thread();
+                const uint32_t c = i * NT + G::thread();
                 if (c < n) f(fresh(i), head + c * E);
             }
-        for (uint32_t c = NV * NT + Group<NT>::thread(); c < n; c += NT) f(words[c], head + c * E);
+        for (uint32_t c = NV * NT + G::thread(); c < n; c += NT) f(words[c], head + c * E);
     }
-    // f(element, its position): all words once more from memory
-    template <class F> __device__ void elements_again(F f) const
+    // the same from memory, in a loop: for what hardly ever runs
+    template <class F> __device__ void again_at(F f) const
     {
 #pragma unroll 1
-        for (uint32_t c = Group<NT>::thread(); c < n; c += NT) {
-            float x[E];
-            P::open(words[c], x);
-#pragma unroll
-            for (int i = 0; i < E; ++i) f(x[i], head + c * E + i);
-        }
-        if (at != 0xffffffffu) f(edge, at);
+        for (uint32_t c = G::thread(); c < n; c += NT) f(words[c], head + c * E);
     }
-    __device__ float max()
+    // f(element, its position), from memory
+    template <class F> __device__ void elements_again(F f) const
     {
-        float m = edge;
-        each([&](Word4 w) {
+        again_at([&](Word4 w, uint32_t v) {
             float x[E];
             P::open(w, x);
 #pragma unroll
-            for (int i = 0; i < E; i += 2) m = max3(m, x[i], x[i + 1]);
+            for (int i = 0; i < E; ++i) f(x[i], v + i);
         });
-        return m;
+        if (at != 0xffffffffu) f(edge, at);
     }
-    // sum exp2((x - base) * scale).  The difference is rounded before the product, so that a row of the type's lowest value
-    // gives 0 and not inf - inf.
-    __device__ float sum(float base, float scale)
+    // Statistics of a wavefront's elements, and `mine`: the maximum of this thread's.
+    // One pass, while the words arrive: exp2 of x * scale less a whole number next to the maximum of the first words, which
+    // costs one rounding and needs no maximum of the row.  Where the true maximum turns out to be far from it, or far from 0,
+    // the sum is made again.
+    __device__ Stats stats(float scale, float &mine)
     {
-        float s = __builtin_amdgcn_exp2f((edge - base) * scale);
+        float m = edge;
+        if (NV > 1) {
+            float x[E];
+            P::open(held[0], x);
+#pragma unroll
+            for (int i = 0; i < E; i += 2) m = max3(m, x[i], x[i + 1]);
+            m = across<Max, G::LANES>(m);
+        } else {
+            each([&](Word4 w) {
+                float x[E];
+                P::open(w, x);
+#pragma unroll
+                for (int i = 0; i < E; i += 2) m = max3(m, x[i], x[i + 1]);
+            });
+            mine = m;
+            m = across<Max, G::LANES>(m);
+        }
+        const float first = m * scale, base = fabsf(first) < FAR ? __builtin_rintf(first) : 0.0f;
+        float s = __builtin_amdgcn_exp2f(__builtin_fmaf(edge, scale, -base)), most = edge;
         each([&](Word4 w) {
             float x[E], part = 0;
             P::open(w, x);
+            if (NV > 1)
 #pragma unroll
-            for (int i = 0; i < E; ++i) part += __builtin_amdgcn_exp2f((x[i] - base) * scale);
+                for (int i = 0; i < E; i += 2) most = max3(most, x[i], x[i + 1]);
+#pragma unroll
+            for (int i = 0; i < E; ++i) part += __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -base));
             s += part;
         });
-        return s;
+        if (NV > 1) {
+            mine = most;
+            m = across<Max, G::LANES>(most);
+        }
+        const float top = m * scale;
+        if (fabsf(top) < FAR && fabsf(top - base) <= 64) {
+            s *= __builtin_amdgcn_exp2f(__builtin_fmaf(-m, scale, base));
+        } else if (m != neg_inf()) {
+            s = __builtin_amdgcn_exp2f((edge - m) * scale);
+            again_at([&](Word4 w, uint32_t) {
+                float x[E];
+                P::open(w, x);
+#pragma unroll
+                for (int i = 0; i < E; ++i) s += __builtin_amdgcn_exp2f((x[i] - m) * scale);
+            });
+        }
+        return {m, across<Add, G::LANES>(s)};
+    }
+    // grad = f * exp2((x - m) * scale)
+    __device__ void store(T *out, float m, float scale, float f)
+    {
+        const float top = m * scale;
+        if (fabsf(top) < FAR) {
+            const float base = __builtin_rintf(top), g = f * __builtin_amdgcn_exp2f(__builtin_fmaf(-m, scale, base));
+            each_at([&](Word4 w, uint32_t v) {
+                float x[E];
+                P::open(w, x);
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], scale, -base)) * g;
+                *(Word4Any *)(out + v) = P::close(x);
+            });
+        } else {
+            again_at([&](Word4 w, uint32_t v) {
+                float x[E];
+                P::open(w, x);
+#pragma unroll
+                for (int i = 0; i < E; ++i) x[i] = __builtin_amdgcn_exp2f((x[i] - m) * scale) * f;
+                *(Word4Any *)(out + v) = P::close(x);
+            });
+        }
+        if (at != 0xffffffffu) out[at] = (T)(__builtin_amdgcn_exp2f((edge - m) * scale) * f);
+    }
+    __device__ void clear(T *out)
+    {
+        for (uint32_t c = G::thread(); c < n; c += NT) *(Word4Any *)(out + head + c * E) = Word4{0, 0, 0, 0};
+        if (at != 0xffffffffu) out[at] = (T)0.0f;
     }
 };
 
@@ -267,7 +371,7 @@ template <class T, int NT, int NV>
 __global__ void __launch_bounds__(Group<NT>::SIZE) k_logprobs_at(Rows in, const int32_t *index, uint32_t k, float *out)
 {
     using G = Group<NT>;
-    __shared__ float buf[2][G::WAVES];
+    __shared__ Stats buf[G::WAVES];
     const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + G::row_in_group();
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
     int32_t at[G::SLOTS];
@@ -277,20 +381,21 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_logprobs_at(Rows in, const 
         at[i] = j < k ? index[r * k + j] : -1;
     }
     Row<T, NT, NV> row;
-    row.load((const T *)in.z + r * in.stride, in.classes);
-    float x[G::SLOTS];
+    row.place((const T *)in.z + r * in.stride, in.classes);
+    row.load();
+    float x[G::SLOTS], mine;
 #pragma unroll
     for (int i = 0; i < G::SLOTS; ++i) x[i] = (uint32_t)at[i] < in.classes ? to_float(row.z[at[i]]) : 0.0f;
-    float m = row.max();
-    G::template reduce<Max, 1>(&m, buf[0]);
-    float s = row.sum(m == neg_inf() ? 0.0f : m, LOG2E);
-    G::template reduce<Add, 1>(&s, buf[1]);
-    const float log_s = __logf(s);
+    Stats st = row.stats(LOG2E, mine);
+    G::put(st, buf);
+    G::sync();
+    st = G::get(st, buf, LOG2E);
+    const float log_s = __logf(st.s);
 #pragma unroll
     for (int i = 0; i < G::SLOTS; ++i) {
         const uint32_t j = i * NT + G::thread();
         float lp = 0;
-        if ((uint32_t)at[i] < in.classes) lp = x[i] == neg_inf() && s == s ? neg_inf() : (x[i] - m) - log_s;
+        if ((uint32_t)at[i] < in.classes) lp = x[i] == neg_inf() && st.s == st.s ? neg_inf() : (x[i] - st.m) - log_s;
         if (j < k) out[r * k + j] = lp;
     }
 }
@@ -313,8 +418,8 @@ __device__ inline float value_of(uint32_t order)
 // order and position in one key: of equal values the lower class is the larger key; no two keys of a row are alike
 __device__ inline uint64_t key_of(float x, uint32_t v) { return (uint64_t)order_of(x) << 32 | (0xffffffffu - v); }
 
-// The largest number t of the given leading bits with ballots for `count` of the keys at or above it, among the keys of all
-// threads of the group's wavefront (N keys to a thread); 0 if there are not as many keys above 0.
+// The largest number t of the given leading bits that at least `count` of the keys reach, among the keys of the group's lanes
+// of a wavefront (N keys to a lane); 0 if there are not as many keys above 0.
 template <int NT, int BITS, int N> __device__ inline uint32_t nth_largest(const uint32_t *keys, uint32_t count)
 {
     uint32_t t = 0;
@@ -323,9 +428,10 @@ template <int NT, int BITS, int N> __device__ inline uint32_t nth_largest(const 
         uint32_t above = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const uint64_t b = __ballot(keys[i] >= (t | bit));
-            above += NT >= 64 ? (uint32_t)__popcll(b) : (uint32_t)__popc((uint32_t)(b >> (threadIdx.x & 63 & ~(NT - 1))) & ((1u << (NT & 31)) - 1));
+            const bool yes = keys[i] >= (t | bit);
+            above += NT >= 64 ? (uint32_t)__popcll(__ballot(yes)) : yes;
         }
+        if (NT < 64) above = across<Add, Group<NT>::LANES>(above);
         if (above >= count) t |= bit;
     }
     return t;
@@ -385,23 +491,24 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
     using G = Group<NT>;
     using P = Pack<T>;
     constexpr int BITS = OrderBits<T>::N, ROOM = NT < 64 ? 128 : CANDIDATES;
-    __shared__ float buf[2][G::WAVES];
+    __shared__ Stats buf[G::WAVES];
     __shared__ uint32_t bounds[G::WAVES], found[G::ROWS], words;
     __shared__ __align__(16) uint64_t best[G::ROWS][ROOM];
-    const uint32_t group = G::row_in_group(), wave = NT > 64 ? threadIdx.x >> 6 : 0;
+    const uint32_t group = G::row_in_group();
     const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + group;
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
     Row<T, NT, NV> row;
-    row.load((const T *)in.z + r * in.stride, in.classes);
-    const float mine = row.max();
-    float m = mine;
+    row.place((const T *)in.z + r * in.stride, in.classes);
+    row.load();
     if (G::thread() == 0) found[group] = 0;
     if (threadIdx.x == 0) words = 0;
-    G::template reduce<Max, 1>(&m, buf[0]);
+    float mine;
+    Stats st = row.stats(LOG2E, mine);
     // wavefronts that have a word for every lane, or the only one
     const uint32_t full = NT <= 64 ? 1 : row.n / 64 < G::WAVES ? row.n / 64 : G::WAVES, each = (k + full - 1) / full;
+    const uint32_t maxima = row.n < NT ? row.n : NT;
     uint32_t bound;
-    if (NV <= 4 && 4 * k > (row.n < NT ? row.n : NT)) {
+    if (NV <= 4 && k > (NT < 64 ? maxima : maxima / 2)) {
         uint32_t keys[NV * P::E + 1];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -416,16 +523,15 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         const uint32_t key = order_of(mine);
         bound = nth_largest<NT, BITS, 1>(&key, each);
     }
-    if (NT > 64) {
-        if ((threadIdx.x & 63) == 0) bounds[wave] = wave < full ? bound : 0xffffffffu;
-    }
-    float s = row.sum(m == neg_inf() ? 0.0f : m, LOG2E);
-    G::template reduce<Add, 1>(&s, buf[1]);
+    G::put(st, buf);
+    if (NT > 64 && (threadIdx.x & 63) == 0) bounds[G::wave()] = G::wave() < full ? bound : 0xffffffffu;
+    G::sync();
+    st = G::get(st, buf, LOG2E);
     if (NT > 64) {
         bound = bounds[0];
         for (int i = 1; i < G::WAVES; ++i) bound = bounds[i] < bound ? bounds[i] : bound;
     }
-    const float log_s = __logf(s);
+    const float log_s = __logf(st.s), m = st.m;
     // the least finite value leaves out -inf and NaN
     const float least = bound ? value_of(bound) : -3.402823466e38f;
     auto keep = [&](float x, uint32_t v) {
@@ -513,6 +619,8 @@ template <int NT> struct Taught {
     float u[G::ROWS][G::TOP];
     int32_t place[G::ROWS][PLACES];
     uint32_t twice[G::ROWS];
+    Stats stats[G::WAVES];
+    float loss[G::WAVES];
 
     __device__ void clear(uint32_t group)
     {
@@ -521,11 +629,13 @@ template <int NT> struct Taught {
     }
 };
 
-// The teacher's slots j of a row, slot j with thread j % NT: class (-1: empty) and answer s_j / T.
+// The teacher's slots j of a row, slot j with thread j % NT: class (-1: empty) and answer t = s_j / T, and their softmax:
+// u = exp(t - m) for the largest t of the wavefront, later of the row.
 template <int NT> struct Slots {
     using G = Group<NT>;
     int32_t v[G::SLOTS];
     float t[G::SLOTS], u[G::SLOTS];
+    Stats st;
 
     __device__ void load(const Answers &a, uint64_t r, uint32_t classes)
     {
@@ -544,25 +654,20 @@ template <int NT> struct Slots {
             }
         }
     }
-    __device__ float max() const
+    // u and its sum within the wavefront; and whether a class comes twice: of two slots of a class one finds the other in a
+    // table of twice as many places as slots.  (All slots going through all others took 0.03 us a slot, 90 us instead of 63
+    // for gradients of 512 x 65537 with 250 slots.)
+    __device__ void weigh(Taught<NT> &lds, uint32_t group)
     {
-        float m = neg_inf();
+        float m = neg_inf(), sum = 0;
 #pragma unroll
         for (int i = 0; i < G::SLOTS; ++i) m = fmaxf(m, t[i]);
-        return m;
-    }
-    // u = exp(t - base), 0 in empty slots; returns their sum.  Leaves classes and u in LDS, and there whether a class comes
-    // twice: of two slots of a class one finds the other in a table of twice as many places as slots.
-    __device__ float weigh(float base, uint32_t k, Taught<NT> &lds, uint32_t group)
-    {
-        float sum = 0;
-        if (NT <= 64) G::sync();                    // others have met a barrier since the table was cleared
+        m = across<Max, G::LANES>(m);
 #pragma unroll
         for (int i = 0; i < G::SLOTS; ++i) {
             u[i] = 0;
             if (v[i] < 0) continue;
-            t[i] -= base;
-            u[i] = __builtin_amdgcn_exp2f(t[i] * LOG2E);
+            u[i] = __builtin_amdgcn_exp2f((t[i] - m) * LOG2E);
             sum += u[i];
             constexpr uint32_t LAST = Taught<NT>::PLACES - 1;
             uint32_t h = ((uint32_t)v[i] * 0x9e3779b1u) >> 16 & LAST;
@@ -573,15 +678,46 @@ template <int NT> struct Slots {
                 h = (h + 1) & LAST;
             }
         }
+        st = {m, across<Add, G::LANES>(sum)};
+        G::put(st, lds.stats);
+    }
+    // After a barrier: u and its sum for the row.
+    __device__ void join(uint32_t k, Taught<NT> &lds, uint32_t group)
+    {
+        const Stats all = G::get(st, lds.stats, LOG2E);
+        const float f = all.m == st.m ? 1.0f : __builtin_amdgcn_exp2f((st.m - all.m) * LOG2E);
+        st = all;
 #pragma unroll
         for (int i = 0; i < G::SLOTS; ++i) {
+            if (NT > 64) u[i] = v[i] >= 0 ? u[i] * f : 0.0f;
             const uint32_t j = i * NT + G::thread();
             if (j < k) {
                 lds.v[group][j] = v[i];
                 lds.u[group][j] = u[i];
             }
         }
-        return sum;
+    }
+    // sum_j p_j (log p_j - (z_j / T - lse)) = A / U - log U + log S with the sum A of u_j (t_j - m - (z_j - m_z) / T); A by
+    // wavefronts
+    __device__ void part_of_loss(const float *x, Stats z, float inv_t, Taught<NT> &lds)
+    {
+        float sum = 0;
+#pragma unroll
+        for (int i = 0; i < G::SLOTS; ++i)
+            if (u[i] != 0.0f) sum += u[i] * ((t[i] - st.m) - (x[i] - z.m) * inv_t);
+        sum = across<Add, G::LANES>(sum);
+        if (NT <= 64) st.m = sum;
+        else if ((threadIdx.x & 63) == 0) lds.loss[G::wave()] = sum;
+    }
+    // After a barrier
+    __device__ float loss(Stats z, const Taught<NT> &lds) const
+    {
+        float sum = st.m;
+        if (NT > 64) {
+            sum = 0;
+            for (uint32_t i = 0; i < (G::WAVES < 4 ? G::WAVES : 4); ++i) sum += lds.loss[i];      // 256 slots
+        }
+        return sum / st.s - __logf(st.s) + __logf(z.s);
     }
     // The u of slot i, or where classes come twice those of all slots of its class, added up in slot order: each of them is
     // stored with the same value.
@@ -594,118 +730,94 @@ template <int NT> struct Slots {
     }
 };
 
-template <class T> __device__ inline void clear_row(T *out, uint32_t n, uint32_t t, uint32_t step)
-{
-    for (uint32_t v = t; v < n; v += step) out[v] = (T)0.0f;
-}
-
-// One pass over a row that stays in registers: its maximum m and S = sum exp((z - m) / T), then loss and gradient.  With
-// u_j = exp(t_j - t_max), U their sum, the three sums S, U and A = sum_j u_j (t_j - t_max - (z_j - m) / T) come out of one
-// reduction, and loss = A / U - log U + log S.
+// A row that stays in registers between its statistics and its gradient.
 template <class T, int NT, int NV, bool GRAD>
 __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a, float *loss, float *lse, T *grad, uint64_t grad_stride)
 {
     using G = Group<NT>;
-    using P = Pack<T>;
-    __shared__ float buf[5 * G::WAVES];
+    __shared__ Stats buf[G::WAVES];
     __shared__ Taught<NT> taught;
     const uint32_t group = G::row_in_group();
     const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + group;
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
     const float w = a.weight ? a.weight[r] : 1.0f, scale = a.inv_t * LOG2E;
     T *out = GRAD ? grad + r * grad_stride : nullptr;
-    float m[2] = {neg_inf(), neg_inf()}, s[3] = {0, 0, 0};
-    Row<T, NT, NV> row;
     Slots<NT> slots;
-    float x[G::SLOTS];
-    taught.clear(group);
-    if (w != 0.0f) {
-        slots.load(a, r, in.classes);
-        row.load((const T *)in.z + r * in.stride, in.classes);
-#pragma unroll
-        for (int i = 0; i < G::SLOTS; ++i) x[i] = slots.v[i] >= 0 ? to_float(row.z[slots.v[i]]) : 0.0f;
-        m[1] = slots.max();
-        m[0] = row.max();
-        G::template reduce<Max, 2>(m, buf);
-        s[1] = slots.weigh(m[1], a.k, taught, group);
-        const float base = m[0] == neg_inf() ? 0.0f : m[0];
-        s[0] = row.sum(base, scale);
-#pragma unroll
-        for (int i = 0; i < G::SLOTS; ++i) {
-            x[i] -= base;
-            if (slots.u[i] != 0.0f) s[2] += slots.u[i] * (slots.t[i] - x[i] * a.inv_t);
-        }
-        G::template reduce<Add, 3>(s, buf + 2 * G::WAVES);
+    Row<T, NT, NV> row;
+    slots.load(a, r, in.classes);
+    row.place((const T *)in.z + r * in.stride, in.classes);
+    // Padding is not read, where reading takes longer than waiting for the weight.
+    if (NT > 64 && w == 0.0f) {
+        if (threadIdx.x == 0) loss[r] = lse[r] = 0;
+        if (GRAD) row.clear(out);
+        return;
     }
-    // neither a filled slot nor a weight, or all logits -inf
-    const bool none = s[1] == 0.0f, excluded = !none && s[0] == 0.0f;
+    row.load();
+    float x[G::SLOTS], mine;
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i) x[i] = slots.v[i] >= 0 ? to_float(row.z[slots.v[i]]) : 0.0f;
+    taught.clear(group);
+    G::sync();
+    slots.weigh(taught, group);
+    Stats st = row.stats(scale, mine);
+    G::put(st, buf);
+    G::sync();
+    st = G::get(st, buf, scale);
+    slots.join(a.k, taught, group);
+    // neither a weight nor a filled slot, or all logits -inf
+    const bool none = w == 0.0f || slots.st.s == 0.0f, excluded = !none && st.s == 0.0f;
     if (none || excluded) {
         if (G::thread() == 0) {
             loss[r] = 0;
             lse[r] = none ? 0.0f : neg_inf();
         }
-        if (GRAD) clear_row(out, in.classes, G::thread(), NT);
+        if (GRAD) row.clear(out);
         return;
     }
-    const float log_s = __logf(s[0]);
-    if (G::thread() == 0) {
-        loss[r] = w * (s[2] / s[1] - __logf(s[1]) + log_s);
-        lse[r] = m[0] * a.inv_t + log_s;
-    }
-    if (!GRAD) return;
-    const float g = w * a.inv_t, gs = g / s[0], gu = g / s[1];
-    row.each_at([&](Word4 words, uint32_t v) {
-        float y[P::E];
-        P::open(words, y);
-#pragma unroll
-        for (int i = 0; i < P::E; ++i) y[i] = __builtin_amdgcn_exp2f((y[i] - m[0]) * scale) * gs;
-        *(Word4Any *)(out + v) = P::close(y);
-    });
-    if (row.at != 0xffffffffu) out[row.at] = (T)(__builtin_amdgcn_exp2f((row.edge - m[0]) * scale) * gs);
-    // the teacher's classes, over the dense part
+    const float g = w * a.inv_t, gs = g / st.s, gu = g / slots.st.s;
+    slots.part_of_loss(x, st, a.inv_t, taught);
+    if (GRAD) row.store(out, st.m, scale, gs);
     G::sync();
+    if (G::thread() == 0) {
+        loss[r] = w * slots.loss(st, taught);
+        lse[r] = st.m * a.inv_t + __logf(st.s);
+    }
+    // the teacher's classes, over the dense part
+    if (GRAD)
 #pragma unroll
-    for (int i = 0; i < G::SLOTS; ++i)
-        if (slots.v[i] >= 0)
-            out[slots.v[i]] = (T)(__builtin_amdgcn_exp2f(x[i] * scale) * gs - slots.of_class(i, a.k, taught, group) * gu);
+        for (int i = 0; i < G::SLOTS; ++i)
+            if (slots.v[i] >= 0)
+                out[slots.v[i]] = (T)(__builtin_amdgcn_exp2f((x[i] - st.m) * scale) * gs - slots.of_class(i, a.k, taught, group) * gu);
 }
 
 // Rows of which there are few, or which no workgroup can hold, are cut into parts of `per` words, a workgroup of 256 to each.
 struct Parts {
     uint32_t count, per;
-    float2 *stats;          // [rows][count]: maximum and sum of every part
+    Stats *stats;           // [rows][count]
 };
 
 template <class T, int NV> __global__ void __launch_bounds__(256) k_part_stats(Rows in, Parts parts, float scale)
 {
     using G = Group<256>;
-    __shared__ float buf[2][G::WAVES];
+    __shared__ Stats buf[G::WAVES];
     const uint64_t r = blockIdx.x / parts.count;
     const uint32_t part = blockIdx.x % parts.count;
     Row<T, 256, NV> row;
-    row.load((const T *)in.z + r * in.stride, in.classes, part * parts.per, parts.per);
-    float m = row.max();
-    G::reduce<Max, 1>(&m, buf[0]);
-    float s = row.sum(m == neg_inf() ? 0.0f : m, scale);
-    G::reduce<Add, 1>(&s, buf[1]);
-    if (threadIdx.x == 0) parts.stats[blockIdx.x] = make_float2(m, s);
+    row.place((const T *)in.z + r * in.stride, in.classes, part * parts.per, parts.per);
+    row.load();
+    float mine;
+    Stats st = row.stats(scale, mine);
+    G::put(st, buf);
+    G::sync();
+    st = G::get(st, buf, scale);
+    if (threadIdx.x == 0) parts.stats[blockIdx.x] = st;
 }
 
-// A thread's share of a row's parts, at most 256 parts: the maximum, then with the row's maximum its sum.
-struct Joined {
-    float m, s;
-    __device__ void load(const Parts &parts, uint64_t r)
-    {
-        m = neg_inf();
-        s = 0;
-        if (threadIdx.x < parts.count) {
-            const float2 v = parts.stats[r * parts.count + threadIdx.x];
-            m = v.x;
-            s = v.y;
-        }
-    }
-    __device__ float sum(float base, float scale) const { return s == 0.0f ? 0.0f : s * __builtin_amdgcn_exp2f((m - base) * scale); }
-};
+// A row's parts, at most 256, to a wavefront's statistics: one part to a thread of a workgroup of 256.
+__device__ inline Stats load_parts(const Parts &parts, uint64_t r)
+{
+    return threadIdx.x < parts.count ? parts.stats[r * parts.count + threadIdx.x] : Stats{neg_inf(), 0.0f};
+}
 
 // The gradient of a part of a row, or with NT < 256 of a whole one, from its statistics: the lse of an earlier call, or with
 // SPLIT the sums of its parts, where part 0 writes loss and lse as well.  Every part weighs the teacher's slots by itself and
@@ -716,77 +828,68 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
 {
     using G = Group<NT>;
     using P = Pack<T>;
-    __shared__ float buf[5 * G::WAVES];
+    __shared__ Stats buf[G::WAVES];
     __shared__ Taught<NT> taught;
     const uint32_t group = G::row_in_group(), count = GRAD ? parts.count : 1;
     const uint32_t part = NT < 256 ? 0 : blockIdx.x % count;
     const uint64_t r = in.first + (NT < 256 ? (uint64_t)blockIdx.x * G::ROWS + group : blockIdx.x / count);
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
-    const float w = a.weight ? a.weight[r] : 1.0f, scale = a.inv_t * LOG2E;
+    const float w = a.weight ? a.weight[r] : 1.0f, scale = a.inv_t * LOG2E, l = SPLIT ? 0.0f : lse[r];
     T *out = GRAD ? grad + r * grad_stride : nullptr;
-    const float l = SPLIT ? 0.0f : lse[r];
-    float m[2] = {neg_inf(), neg_inf()}, s[3] = {0, 0, 0};
-    Row<T, NT, NV> row;
+    const T *z = (const T *)in.z + r * in.stride;
     Slots<NT> slots;
-    Joined joined;
+    Row<T, NT, NV> row;
+    Stats st = {0.0f, 1.0f};
+    slots.load(a, r, in.classes);
+    if (SPLIT) st = load_parts(parts, r);
+    if (GRAD) {
+        row.place(z, in.classes, part * parts.per, parts.per);
+        row.load();
+    }
     float x[G::SLOTS];
+#pragma unroll
+    for (int i = 0; i < G::SLOTS; ++i) x[i] = slots.v[i] >= 0 ? to_float(z[slots.v[i]]) : 0.0f;
     taught.clear(group);
-    const bool wanted = w != 0.0f && l != neg_inf();
-    if (wanted) {
-        slots.load(a, r, in.classes);
-        if (SPLIT) joined.load(parts, r);
+    G::sync();
+    slots.weigh(taught, group);
+    if (SPLIT) {
+        st = st.together<G::LANES>(scale);
+        G::put(st, buf);
     }
-    if (GRAD) row.load((const T *)in.z + r * in.stride, in.classes, part * parts.per, parts.per);
-    if (wanted) {
-#pragma unroll
-        for (int i = 0; i < G::SLOTS; ++i)
-            x[i] = slots.v[i] >= 0 ? to_float(((const T *)in.z + r * in.stride)[slots.v[i]]) : 0.0f;
-        m[1] = slots.max();
-        if (SPLIT) {
-            m[0] = joined.m;
-            G::template reduce<Max, 2>(m, buf);
-        } else {
-            G::template reduce<Max, 1>(m + 1, buf);
+    G::sync();
+    if (SPLIT) st = G::get(st, buf, scale);
+    slots.join(a.k, taught, group);
+    const bool none = w == 0.0f || slots.st.s == 0.0f, excluded = SPLIT ? !none && st.s == 0.0f : l == neg_inf();
+    if (none || excluded) {
+        if (SPLIT && part == 0 && threadIdx.x == 0) {
+            loss[r] = 0;
+            lse[r] = none ? 0.0f : neg_inf();
         }
-        s[1] = slots.weigh(m[1], a.k, taught, group);
-        if (SPLIT) {
-            if (m[0] == neg_inf()) m[0] = 0;
-            s[0] = joined.sum(m[0], scale);
-#pragma unroll
-            for (int i = 0; i < G::SLOTS; ++i)
-                if (slots.u[i] != 0.0f) s[2] += slots.u[i] * (slots.t[i] - (x[i] - m[0]) * a.inv_t);
-            G::template reduce<Add, 3>(s, buf + 2 * G::WAVES);
-        } else {
-            G::template reduce<Add, 1>(s + 1, buf + 2 * G::WAVES);
-        }
-    }
-    const bool none = s[1] == 0.0f, excluded = SPLIT && !none && s[0] == 0.0f, zero = none || excluded;
-    if (SPLIT && part == 0 && G::thread() == 0) {
-        const float log_s = __logf(s[0]);
-        loss[r] = zero ? 0.0f : w * (s[2] / s[1] - __logf(s[1]) + log_s);
-        lse[r] = none ? 0.0f : excluded ? neg_inf() : m[0] * a.inv_t + log_s;
-    }
-    if (!GRAD) return;
-    // the row's share: what is taken off z / T, and the factor of exp
-    const float g = w * a.inv_t, gu = g / s[1], gs = zero ? 0.0f : SPLIT ? g / s[0] : g;
-    auto student = [&](float z) {
-        // z / T is not rounded before lse is taken off
-        return __builtin_amdgcn_exp2f(SPLIT ? (z - m[0]) * scale : __builtin_fmaf(z, a.inv_t, -l) * LOG2E) * gs;
-    };
-    if (zero) {
-        row.each_at([&](Word4, uint32_t v) { *(Word4Any *)(out + v) = Word4{0, 0, 0, 0}; });
-        if (row.at != 0xffffffffu) out[row.at] = (T)0.0f;
+        if (GRAD) row.clear(out);
         return;
     }
-    row.each_at([&](Word4 words, uint32_t v) {
-        float y[P::E];
-        P::open(words, y);
+    const float g = w * a.inv_t, gs = g / st.s, gu = g / slots.st.s;
+    // z / T is not rounded before lse is taken off
+    auto student = [&](float z) {
+        return __builtin_amdgcn_exp2f(SPLIT ? (z - st.m) * scale : __builtin_fmaf(z, a.inv_t, -l) * LOG2E) * gs;
+    };
+    if (SPLIT && part == 0) slots.part_of_loss(x, st, a.inv_t, taught);
+    if (GRAD) {
+        row.each_at([&](Word4 words, uint32_t v) {
+            float y[P::E];
+            P::open(words, y);
 #pragma unroll
-        for (int i = 0; i < P::E; ++i) y[i] = student(y[i]);
-        *(Word4Any *)(out + v) = P::close(y);
-    });
-    if (row.at != 0xffffffffu) out[row.at] = (T)student(row.edge);
+            for (int i = 0; i < P::E; ++i) y[i] = student(y[i]);
+            *(Word4Any *)(out + v) = P::close(y);
+        });
+        if (row.at != 0xffffffffu) out[row.at] = (T)student(row.edge);
+    }
     G::sync();
+    if (SPLIT && part == 0 && threadIdx.x == 0) {
+        loss[r] = w * slots.loss(st, taught);
+        lse[r] = st.m * a.inv_t + __logf(st.s);
+    }
+    if (!GRAD) return;
     // part 0 has the edges too: all classes before its words, and those behind the last part's
     const uint32_t end = row.head + row.n * P::E, words_end = in.classes - (in.classes - row.head) % P::E;
 #pragma unroll
@@ -801,20 +904,17 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
 template <class T> __global__ void __launch_bounds__(256) k_part_logprobs(Rows in, Parts parts, const int32_t *index, uint32_t k, float *out)
 {
     using G = Group<256>;
-    __shared__ float buf[2][G::WAVES];
+    __shared__ Stats buf[G::WAVES];
     const uint64_t r = blockIdx.x;
-    const T *z = (const T *)in.z + r * in.stride;
-    Joined joined;
-    joined.load(parts, r);
     const uint32_t j = threadIdx.x;
     const int32_t at = j < k ? index[r * k + j] : -1;
+    Stats st = load_parts(parts, r).together<64>(LOG2E);
     const bool filled = (uint32_t)at < in.classes;
-    const float x = filled ? to_float(z[at]) : 0.0f;
-    float m = joined.m;
-    G::reduce<Max, 1>(&m, buf[0]);
-    float s = joined.sum(m == neg_inf() ? 0.0f : m, LOG2E);
-    G::reduce<Add, 1>(&s, buf[1]);
-    if (j < k) out[r * k + j] = !filled ? 0.0f : x == neg_inf() && s == s ? neg_inf() : (x - m) - __logf(s);
+    const float x = filled ? to_float(((const T *)in.z + r * in.stride)[at]) : 0.0f;
+    G::put(st, buf);
+    G::sync();
+    st = G::get(st, buf, LOG2E);
+    if (j < k) out[r * k + j] = !filled ? 0.0f : x == neg_inf() && st.s == st.s ? neg_inf() : (x - st.m) - __logf(st.s);
 }
 
 }  // namespace answers
