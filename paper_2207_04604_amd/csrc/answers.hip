@@ -71,9 +71,12 @@ template <class F> d2mhe_status with_shape(const d2mhe_logits *z, uint32_t k, F 
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
         if (words <= 16 && k <= Group<16>::TOP) f(zero, Shape<16, 1>());
-        else if (words <= 128) f(zero, Shape<64, 2>());
+        else if (words <= 64 && k <= Group<16>::TOP) f(zero, Shape<16, 4>());
+        else if (words <= 128 && k <= Group<16>::TOP) f(zero, Shape<16, 8>());
+        else if (words <= 512) f(zero, Shape<64, 8>());
         else if (words <= 1024) f(zero, Shape<256, 4>());
-        else if (words <= 4096) f(zero, Shape<256, 16>());
+        else if (words <= 2048) f(zero, Shape<256, 8>());
+        else if (words <= 4096) f(zero, Shape<512, 8>());
         else if (words <= 8192) f(zero, Shape<512, 16>());
         else f(zero, Shape<1024, 16>());
     });
@@ -135,12 +138,13 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
             hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in, k, index, logprob);
         });
     };
-    // 16 threads have 16 maxima, which leaves few candidates to up to four slots; the 256 threads of a row of more than 1024
-    // words have room for a quarter of their maxima
+    // as many threads as give a close bound: four maxima to a slot, two in a wavefront by itself
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
         if (words <= 16 && k <= 16) run(zero, Shape<16, 1>());
+        else if (words <= 64 && k <= 16) run(zero, Shape<16, 4>());
         else if (words <= 128) run(zero, Shape<64, 2>());
+        else if (words <= 512 && k <= 32) run(zero, Shape<64, 8>());
         else if (words <= 1024) run(zero, Shape<256, 4>());
         else if (words <= 4096 && k <= 64) run(zero, Shape<256, 16>());
         else if (words <= 4096) run(zero, Shape<1024, 4>());
@@ -235,8 +239,11 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
     };
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
-        if (words <= 16 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 1>(), Parts{1, words, nullptr});
-        else if (words <= 128) run(zero, Shape<64, 2>(), Parts{1, words, nullptr});
+        const Parts whole = {1, words, nullptr};
+        if (words <= 16 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 1>(), whole);
+        else if (words <= 64 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 4>(), whole);
+        else if (words <= 128) run(zero, Shape<64, 2>(), whole);
+        else if (words <= 384) run(zero, Shape<64, 8>(), whole);
         else run(zero, Shape<256, 4>(), Parts{(words + PART_WORDS - 1) / PART_WORDS, PART_WORDS, nullptr});
     });
 }

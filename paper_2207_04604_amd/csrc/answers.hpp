@@ -4,6 +4,8 @@
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "../../include/d2mhe.h"
 
 namespace d2 {
@@ -415,11 +417,32 @@ __device__ inline float value_of(uint32_t order)
     return __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order);
 }
 
-// order and position in one key: of equal values the lower class is the larger key; no two keys of a row are alike
-__device__ inline uint64_t key_of(float x, uint32_t v) { return (uint64_t)order_of(x) << 32 | (0xffffffffu - v); }
+// Order and position in one key: of equal values the lower class is the larger key, no two keys of a row are alike, and 0 is
+// less than any.  Short rows of 16-bit types have room for both in 32 bits.
+template <class T, class Key> struct Keys {
+    static __device__ Key of(float x, uint32_t v) { return (Key)order_of(x) << 32 | (0xffffffffu - v); }
+    static __device__ float value(Key k) { return value_of((uint32_t)(k >> 32)); }
+    static __device__ int32_t position(Key k) { return (int32_t)(0xffffffffu - (uint32_t)k); }
+};
+template <class T> struct Keys<T, uint32_t> {
+    static __device__ uint32_t of(float x, uint32_t v)
+    {
+        const uint32_t h = __builtin_bit_cast(uint16_t, (T)(x + 0.0f));
+        return (h & 0x8000u ? ~h & 0xffffu : h | 0x8000u) << 16 | (0xffffu - v);
+    }
+    static __device__ float value(uint32_t k)
+    {
+        const uint32_t o = k >> 16;
+        return to_float(__builtin_bit_cast(T, (uint16_t)(o & 0x8000u ? o & 0x7fffu : ~o)));
+    }
+    static __device__ int32_t position(uint32_t k) { return (int32_t)(0xffffu - (k & 0xffffu)); }
+};
+template <class K> struct alignas(16) Four {
+    K k[16 / sizeof(K)];
+};
 
-// The largest number t of the given leading bits that at least `count` of the keys reach, among the keys of the group's lanes
-// of a wavefront (N keys to a lane); 0 if there are not as many keys above 0.
+// A number t that at least `count` of the keys reach, and none but equal ones more, among the keys of the group's lanes of a
+// wavefront (N keys to a lane); 0 if there are not as many keys above 0.  Bit by bit from the top, of the given leading bits.
 template <int NT, int BITS, int N> __device__ inline uint32_t nth_largest(const uint32_t *keys, uint32_t count)
 {
     uint32_t t = 0;
@@ -433,6 +456,7 @@ template <int NT, int BITS, int N> __device__ inline uint32_t nth_largest(const 
         }
         if (NT < 64) above = across<Add, Group<NT>::LANES>(above);
         if (above >= count) t |= bit;
+        if (above == count) break;
     }
     return t;
 }
@@ -446,7 +470,7 @@ constexpr uint32_t CANDIDATES = 1024;
 
 // The k-th largest key digit by digit from the top: the counts of the next eight bits among the keys that agree with the
 // digits chosen so far. For rows with more candidates than LDS has room for, such as many equal values.
-template <int NT, class R> __device__ uint64_t least_by_digits(R &row, uint32_t k, uint32_t *count)
+template <class T, int NT, class R> __device__ uint64_t least_by_digits(R &row, uint32_t k, uint32_t *count)
 {
     __shared__ uint64_t least;
     __shared__ uint32_t need, done;
@@ -462,7 +486,7 @@ template <int NT, class R> __device__ uint64_t least_by_digits(R &row, uint32_t 
         if (done) break;
         const uint64_t prefix = least;
         row.elements_again([&](float x, uint32_t v) {
-            const uint64_t key = key_of(x, v);
+            const uint64_t key = Keys<T, uint64_t>::of(x, v);
             if ((key >> 32) && (shift == 56 || (key >> (shift + 8)) == (prefix >> (shift + 8))))
                 atomicAdd(&count[(key >> shift) & 255], 1u);
         });
@@ -481,6 +505,65 @@ template <int NT, class R> __device__ uint64_t least_by_digits(R &row, uint32_t 
     return least;
 }
 
+// The same within a wavefront: the k-th largest value, and among those equal to it the position of the last to be chosen, bit by
+// bit with ballots. Stores the k best keys (all, if there are fewer) and returns their number.
+template <class T, int NT, int NV, int BITS, class R, class Key> __device__ uint32_t best_of_many(R &row, uint32_t k, Key *best)
+{
+    using P = Pack<T>;
+    constexpr uint32_t MASK = BITS == 32 ? 0xffffffffu : ~(0xffffffffu >> BITS);
+    auto count = [&](auto f) {
+        uint32_t n = 0;
+        row.each([&](Word4 w) {
+            float x[P::E];
+            P::open(w, x);
+#pragma unroll
+            for (int e = 0; e < P::E; ++e) n += (uint32_t)__popcll(__ballot(f(x[e], e)));
+        });
+        return n + (uint32_t)__popcll(__ballot(f(row.edge, P::E)));
+    };
+    uint32_t t = 0;
+#pragma unroll 1
+    for (uint32_t bit = 0x80000000u; bit & MASK; bit >>= 1)
+        if (count([&](float x, int) { return order_of(x) >= (t | bit); }) >= k) t |= bit;
+    // equal ones from the lowest position on: up to which
+    const uint32_t left = k - count([&](float x, int) { return (order_of(x) & MASK) > t; });
+    uint32_t low = 0, high = 0xffffffffu;
+#pragma unroll 1
+    while (t && low < high) {
+        const uint32_t mid = low + (high - low) / 2;
+        uint32_t n = 0;
+        row.each_at([&](Word4 w, uint32_t v) {
+            float x[P::E];
+            P::open(w, x);
+#pragma unroll
+            for (int e = 0; e < P::E; ++e) n += (order_of(x[e]) & MASK) == t && v + e <= mid;
+        });
+        n += row.at != 0xffffffffu && (order_of(row.edge) & MASK) == t && row.at <= mid;
+        if (across<Add, 64>(n) >= left) high = mid;
+        else low = mid + 1;
+    }
+    uint32_t n = 0;
+    const uint64_t below = (1ull << (threadIdx.x & 63)) - 1;
+    auto keep = [&](float x, uint32_t v, bool has) {
+        const uint32_t o = order_of(x) & MASK;
+        const bool yes = has && order_of(x) && (o > t || (o == t && v <= high));
+        const uint64_t b = __ballot(yes);
+        if (yes) best[n + __popcll(b & below)] = Keys<T, Key>::of(x, v);
+        n += (uint32_t)__popcll(b);
+    };
+#pragma unroll 1
+    for (uint32_t c = 0; c < row.n; c += NT) {
+        const bool has = c + (threadIdx.x & 63) < row.n;
+        float x[P::E];
+        P::open(has ? row.words[c + (threadIdx.x & 63)] : Word4{P::NONE, P::NONE, P::NONE, P::NONE}, x);
+#pragma unroll
+        for (int e = 0; e < P::E; ++e) keep(x[e], row.head + (c + (threadIdx.x & 63)) * P::E + e, has);
+    }
+    keep(row.edge, row.at, row.at != 0xffffffffu);
+    Group<NT>::sync();
+    return n;
+}
+
 // Two rounds over a row in registers.  The first gives the maximum of every thread; the `each`-th largest of a wavefront's
 // maxima, the least of them over the wavefronts, is a bound that at least k elements reach.  (Few words or many slots: the
 // bound comes from the elements themselves.)  The second collects what reaches it, usually little more than k, in LDS, where
@@ -490,10 +573,13 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
 {
     using G = Group<NT>;
     using P = Pack<T>;
-    constexpr int BITS = OrderBits<T>::N, ROOM = NT < 64 ? 128 : CANDIDATES;
+    // rows of at most NT * NV * E elements where NT is not the most
+    using Key = std::conditional_t<NT <= 64 && sizeof(T) == 2, uint32_t, uint64_t>;
+    using K = Keys<T, Key>;
+    constexpr int BITS = OrderBits<T>::N, ROOM = NT > 64 ? CANDIDATES : NT * NV * P::E < 1024 ? NT * NV * P::E : NV > 4 ? 512 : 1024;
     __shared__ Stats buf[G::WAVES];
     __shared__ uint32_t bounds[G::WAVES], found[G::ROWS], words;
-    __shared__ __align__(16) uint64_t best[G::ROWS][ROOM];
+    __shared__ __align__(16) Key best[G::ROWS][ROOM];
     const uint32_t group = G::row_in_group();
     const uint64_t r = in.first + (uint64_t)blockIdx.x * G::ROWS + group;
     if (r >= in.rows) return;                       // NT > 64: the whole workgroup
@@ -537,7 +623,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
     auto keep = [&](float x, uint32_t v) {
         if (x >= least) {
             const uint32_t i = atomicAdd(&found[group], 1u);
-            if (i < ROOM) best[group][i] = key_of(x, v);
+            if (i < ROOM) best[group][i] = K::of(x, v);
         }
     };
     if (row.at != 0xffffffffu) keep(row.edge, row.at);
@@ -547,7 +633,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         for (int i = 1; i + 1 < P::E; i += 2) most = max3(most, x[i], x[i + 1]);
         return max3(most, x[P::E - 1], most) >= least;
     };
-    if constexpr (NV <= 4) {
+    if constexpr (NV <= 4 || NT <= 64) {
         row.each_at([&](Word4 w, uint32_t v) {
             float x[P::E];
             P::open(w, x);
@@ -582,25 +668,28 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
     }
     G::sync();
     uint32_t n = found[group];
+    if constexpr (NT <= 64 && NT * NV * P::E > ROOM) {
+        if (n > ROOM) n = best_of_many<T, NT, NV, BITS>(row, k, best[group]);
+    }
     if (NT > 64 && n > ROOM) {
         __shared__ uint32_t count[256];
-        const uint64_t last = least_by_digits<NT>(row, k, count);
+        const uint64_t last = least_by_digits<T, NT>(row, k, count);
         if (threadIdx.x == 0) found[0] = 0;
         __syncthreads();
         row.elements_again([&](float x, uint32_t v) {
-            const uint64_t key = key_of(x, v);
-            if ((key >> 32) && key >= last) best[0][atomicAdd(&found[0], 1u)] = key;
+            const uint64_t key = Keys<T, uint64_t>::of(x, v);
+            if ((key >> 32) && key >= last) best[0][atomicAdd(&found[0], 1u)] = (Key)key;
         });
         __syncthreads();
         n = found[0];
     }
     for (uint32_t i = G::thread(); i < n; i += NT) {
-        const uint64_t key = best[group][i];
+        const Key key = best[group][i];
         uint32_t place = 0;
         for (uint32_t j = 0; j < n; ++j) place += best[group][j] > key;
         if (place < k) {
-            index[r * k + place] = (int32_t)(0xffffffffu - (uint32_t)key);
-            out[r * k + place] = (value_of((uint32_t)(key >> 32)) - m) - log_s;
+            index[r * k + place] = K::position(key);
+            out[r * k + place] = (K::value(key) - m) - log_s;
         }
     }
     for (uint32_t i = n + G::thread(); i < k; i += NT) {

@@ -19,7 +19,7 @@ GUARD = 1234.0
 
 # rows, classes, elements between rows, k: one class; fewer classes than slots; around a wavefront, a workgroup and a
 # 16-byte word; odd strides; the largest k; rows longer than what a workgroup can hold
-SHAPES = [(1, 1, 0, 1), (3, 2, 0, 5), (256, 10, 0, 10), (5, 63, 1, 7), (67, 64, 0, 64), (5, 65, 3, 65), (700, 257, 0, 3),
+SHAPES = [(1, 1, 0, 1), (3, 2, 0, 5), (256, 10, 0, 10), (5, 63, 1, 7), (67, 64, 0, 64), (5, 65, 3, 65), (700, 257, 0, 3), (9, 509, 3, 16), (130, 1029, 0, 10), (6, 1500, 0, 130), (3, 4097, 1, 30),
           (9, 511, 0, 100), (4, 1000, 24, 17), (33, 1023, 2, 256), (3, 2049, 0, 33), (2, 4099, 5, 250), (5, 8192, 0, 8),
           (2, 12289, 0, 64), (3, 32769, 0, 64), (1, 50001, 0, 16), (40, 50001, 0, 5), (2, 131072, 0, 256), (3, 131081, 7, 31),
           (1, 300007, 0, 64), (600, 20011, 0, 3)]
@@ -196,7 +196,7 @@ def test_gradient_is_that_of_the_loss():
 # ---- values at the ends -----------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", list(TORCH))
-@pytest.mark.parametrize("V,k", [(9, 4), (100, 20), (1000, 100), (5000, 256), (131072, 64)])
+@pytest.mark.parametrize("V,k", [(9, 4), (100, 20), (300, 9), (1000, 100), (1999, 30), (4001, 12), (5000, 256), (131072, 64)])
 def test_equal_logits_go_to_the_lower_class(dtype, V, k):
     rng = np.random.default_rng(V)
     z = rng.integers(-2, 3, (6, V)).astype(np.float32)              # few values, so nearly all are ties
@@ -213,7 +213,7 @@ def test_equal_logits_go_to_the_lower_class(dtype, V, k):
     within(lp, wlp, R.logprob_error(z, wlp))
 
 
-@pytest.mark.parametrize("V,k", [(40, 12), (3000, 256), (70000, 100)])
+@pytest.mark.parametrize("V,k", [(40, 12), (250, 5), (2040, 32), (3000, 256), (70000, 100)])
 def test_all_large_logits_side_by_side(V, k):
     """Increasing and decreasing rows, and rows whose large values all lie in one short run or a fixed distance apart."""
     rng = np.random.default_rng(V)
