@@ -138,13 +138,10 @@ def strerror(status: int) -> str:
 
 def _ptr(buf):
     """Device address of a tensor / array / raw integer (None -> NULL)."""
-    if buf is None:
-        return None
-    if isinstance(buf, int):
-        return buf
-    if hasattr(buf, "data_ptr"):
-        return buf.data_ptr()
-    return buf.ctypes.data
+    try:
+        return buf.data_ptr()               # most buffers are tensors
+    except AttributeError:
+        return buf if buf is None or isinstance(buf, int) else buf.ctypes.data
 
 
 def _ptr_table(bufs):

@@ -56,7 +56,7 @@ template <class F> d2mhe_status with_type(uint32_t dtype, F f)
     return hipGetLastError() == hipSuccess ? D2MHE_OK : D2MHE_ERR_HIP;
 }
 
-constexpr uint32_t SPLIT_ROWS = 192, SPLIT_GROUPS = 512, PART_WORDS = 1024;
+constexpr uint32_t SPLIT_ROWS = 128, SPLIT_WORDS = 8192, SPLIT_GROUPS = 1024, PART_WORDS = 1024;
 
 template <class T> uint32_t words_of(const d2mhe_logits *z) { return (z->classes + Pack<T>::E - 1) / Pack<T>::E; }
 
@@ -87,7 +87,7 @@ Parts parts_of(const d2mhe_logits *z, void *scratch)
 {
     const uint32_t e = z->dtype == D2MHE_F32 ? 4 : 8, words = (z->classes + e - 1) / e;
     Parts p = {1, words, (Stats *)scratch};
-    if (z->rows == 0 || z->rows >= SPLIT_ROWS || words <= PART_WORDS) return p;
+    if (z->rows == 0 || z->rows > SPLIT_ROWS || words <= SPLIT_WORDS) return p;
     uint32_t want = (SPLIT_GROUPS + z->rows - 1) / z->rows;
     const uint32_t most = (words + PART_WORDS - 1) / PART_WORDS;
     if (want > most) want = most;
