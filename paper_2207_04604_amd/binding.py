@@ -138,10 +138,12 @@ def strerror(status: int) -> str:
 
 def _ptr(buf):
     """Device address of a tensor / array / raw integer (None -> NULL)."""
+    if buf is None or isinstance(buf, int):
+        return buf
     try:
-        return buf.data_ptr()               # most buffers are tensors
+        return buf.data_ptr()
     except AttributeError:
-        return buf if buf is None or isinstance(buf, int) else buf.ctypes.data
+        return buf.ctypes.data
 
 
 def _ptr_table(bufs):

@@ -724,6 +724,7 @@ template <int NT> struct Slots {
     using G = Group<NT>;
     int32_t v[G::SLOTS];
     float t[G::SLOTS], u[G::SLOTS];
+    bool own[G::SLOTS];     // the class is in these threads' part of the row
     Stats st;
 
     __device__ void load(const Answers &a, uint64_t r, uint32_t classes)
@@ -741,6 +742,7 @@ template <int NT> struct Slots {
                     t[i] = s * a.inv_members * a.inv_t;
                 }
             }
+            own[i] = v[i] >= 0;
         }
     }
     // u and its sum within the wavefront; and whether a class comes twice: of two slots of a class one finds the other in a
@@ -758,6 +760,7 @@ template <int NT> struct Slots {
             if (v[i] < 0) continue;
             u[i] = __builtin_amdgcn_exp2f((t[i] - m) * LOG2E);
             sum += u[i];
+            if (!own[i]) continue;
             constexpr uint32_t LAST = Taught<NT>::PLACES - 1;
             uint32_t h = ((uint32_t)v[i] * 0x9e3779b1u) >> 16 & LAST;
             while (true) {                          // ends: half of the places stay free
@@ -935,9 +938,16 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
         row.place(z, in.classes, part * parts.per, parts.per);
         row.load();
     }
+    // part 0 has the edges too: all classes before its words, and those behind the last part's
+    const uint32_t end = row.head + row.n * P::E, words_end = in.classes - (in.classes - row.head) % P::E;
     float x[G::SLOTS];
 #pragma unroll
-    for (int i = 0; i < G::SLOTS; ++i) x[i] = slots.v[i] >= 0 ? to_float(z[slots.v[i]]) : 0.0f;
+    for (int i = 0; i < G::SLOTS; ++i) {
+        const uint32_t v = slots.v[i];
+        const bool filled = slots.v[i] >= 0;
+        if (GRAD) slots.own[i] = filled && ((v >= row.head && v < end) || (part == 0 && (v < row.head || v >= words_end)));
+        x[i] = slots.own[i] || (SPLIT && part == 0 && filled) ? to_float(z[v]) : 0.0f;
+    }
     taught.clear(group);
     G::sync();
     slots.weigh(taught, group);
@@ -979,14 +989,9 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
         lse[r] = st.m * a.inv_t + __logf(st.s);
     }
     if (!GRAD) return;
-    // part 0 has the edges too: all classes before its words, and those behind the last part's
-    const uint32_t end = row.head + row.n * P::E, words_end = in.classes - (in.classes - row.head) % P::E;
 #pragma unroll
-    for (int i = 0; i < G::SLOTS; ++i) {
-        const uint32_t v = slots.v[i];
-        if (slots.v[i] >= 0 && ((v >= row.head && v < end) || (part == 0 && (v < row.head || v >= words_end))))
-            out[v] = (T)(student(x[i]) - slots.of_class(i, a.k, taught, group) * gu);
-    }
+    for (int i = 0; i < G::SLOTS; ++i)
+        if (slots.own[i]) out[slots.v[i]] = (T)(student(x[i]) - slots.of_class(i, a.k, taught, group) * gu);
 }
 
 // Log-probabilities of rows whose parts have been summed up.
