@@ -123,10 +123,36 @@ struct Add {
     static __device__ uint32_t of(uint32_t a, uint32_t b) { return a + b; }
 };
 
+struct Min {
+    static __device__ uint32_t of(uint32_t a, uint32_t b) { return a < b ? a : b; }
+};
+
 template <int ROR, class V> __device__ inline V rotated(V v)            // lane l of 16: what lane l - ROR holds
 {
-    const int i = __builtin_bit_cast(int, v);
-    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(i, i, 0x120 + ROR, 0xf, 0xf, false));
+    if constexpr (sizeof(V) == 8) {
+        return (V)rotated<ROR>((uint32_t)(v >> 32)) << 32 | rotated<ROR>((uint32_t)v);
+    } else {
+        const int i = __builtin_bit_cast(int, v);
+        return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(i, i, 0x120 + ROR, 0xf, 0xf, false));
+    }
+}
+
+// how many of the 16 lanes that turn with a lane hold more than it
+template <int R = 15, class V> __device__ inline uint32_t larger_of_16(V v)
+{
+    if constexpr (R == 0) return 0;
+    else return larger_of_16<R - 1>(v) + (rotated<R>(v) > v);
+}
+
+// lane l of 16: the sum of what the lanes before it hold
+__device__ inline uint32_t before_in_16(uint32_t v)
+{
+    uint32_t s = v;
+    s += __builtin_amdgcn_update_dpp(0, s, 0x111, 0xf, 0xf, true);          // from the lane before, 0 in the first
+    s += __builtin_amdgcn_update_dpp(0, s, 0x112, 0xf, 0xf, true);
+    s += __builtin_amdgcn_update_dpp(0, s, 0x114, 0xf, 0xf, true);
+    s += __builtin_amdgcn_update_dpp(0, s, 0x118, 0xf, 0xf, true);
+    return s - v;
 }
 
 // Op over the W neighbouring lanes of a lane, in all of them and to the same bits: rotations within 16 lanes, then exchanges
@@ -594,7 +620,9 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
     const uint32_t full = NT <= 64 ? 1 : row.n / 64 < G::WAVES ? row.n / 64 : G::WAVES, each = (k + full - 1) / full;
     const uint32_t maxima = row.n < NT ? row.n : NT;
     uint32_t bound;
-    if (NV <= 4 && k > (NT < 64 ? maxima : maxima / 2)) {
+    if (NT == 16 && (in.classes <= 16 || (in.classes <= 48 && k > maxima))) {
+        bound = 0;                                  // all of them: fewer comparisons than a search
+    } else if (NV <= 4 && k > (NT < 64 ? maxima : maxima / 2)) {
         uint32_t keys[NV * P::E + 1];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -607,7 +635,9 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         bound = nth_largest<NT, BITS, NV * P::E + 1>(keys, each);
     } else {
         const uint32_t key = order_of(mine);
-        bound = nth_largest<NT, BITS, 1>(&key, each);
+        // of 16 maxima all that fewer than k exceed; 0 if there are not as many
+        if constexpr (NT == 16) bound = across<Min, 16>(larger_of_16(key) < k ? key : 0xffffffffu);
+        else bound = nth_largest<NT, BITS, 1>(&key, each);
     }
     G::put(st, buf);
     if (NT > 64 && (threadIdx.x & 63) == 0) bounds[G::wave()] = G::wave() < full ? bound : 0xffffffffu;
@@ -626,14 +656,37 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
             if (i < ROOM) best[group][i] = K::of(x, v);
         }
     };
-    if (row.at != 0xffffffffu) keep(row.edge, row.at);
+    if (NT != 16 && row.at != 0xffffffffu) keep(row.edge, row.at);
     auto reaches = [&](const float *x) {
         float most = x[0];
 #pragma unroll
         for (int i = 1; i + 1 < P::E; i += 2) most = max3(most, x[i], x[i + 1]);
         return max3(most, x[P::E - 1], most) >= least;
     };
-    if constexpr (NV <= 4 || NT <= 64) {
+    uint32_t taken = 0;
+    if constexpr (NT == 16) {
+        // every lane's places follow from the counts of the lanes before: no atomics, one after the other, for so few
+        uint64_t mine = (uint64_t)(row.edge >= least) << NV * P::E;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[P::E];
+            P::open(row.fresh(i), x);
+#pragma unroll
+            for (int e = 0; e < P::E; ++e) mine |= (uint64_t)(x[e] >= least) << (i * P::E + e);
+        }
+        const uint32_t count = (uint32_t)__popcll(mine);
+        uint32_t at = before_in_16(count);
+        taken = across<Add, 16>(count);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float x[P::E];
+            P::open(row.fresh(i), x);
+#pragma unroll
+            for (int e = 0; e < P::E; ++e)
+                if (mine >> (i * P::E + e) & 1) best[group][at++] = K::of(x[e], row.head + (i * NT + G::thread()) * P::E + e);
+        }
+        if (mine >> NV * P::E) best[group][at] = K::of(row.edge, row.at);
+    } else if constexpr (NV <= 4 || NT <= 64) {
         row.each_at([&](Word4 w, uint32_t v) {
             float x[P::E];
             P::open(w, x);
@@ -667,7 +720,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         }
     }
     G::sync();
-    uint32_t n = found[group];
+    uint32_t n = NT == 16 ? taken : found[group];
     if constexpr (NT <= 64 && NT * NV * P::E > ROOM) {
         if (n > ROOM) n = best_of_many<T, NT, NV, BITS>(row, k, best[group]);
     }
@@ -683,13 +736,21 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         __syncthreads();
         n = found[0];
     }
-    for (uint32_t i = G::thread(); i < n; i += NT) {
-        const Key key = best[group][i];
-        uint32_t place = 0;
-        for (uint32_t j = 0; j < n; ++j) place += best[group][j] > key;
-        if (place < k) {
-            index[r * k + place] = K::position(key);
-            out[r * k + place] = (K::value(key) - m) - log_s;
+    auto put = [&](Key key, uint32_t place) {
+        if (place >= k) return;
+        index[r * k + place] = K::position(key);
+        out[r * k + place] = (K::value(key) - m) - log_s;
+    };
+    if (NT == 16 && n <= 16) {
+        const Key key = G::thread() < n ? best[group][G::thread()] : 0;
+        const uint32_t place = larger_of_16(key);
+        if (G::thread() < n) put(key, place);
+    } else {
+        for (uint32_t i = G::thread(); i < n; i += NT) {
+            const Key key = best[group][i];
+            uint32_t place = 0;
+            for (uint32_t j = 0; j < n; ++j) place += best[group][j] > key;
+            put(key, place);
         }
     }
     for (uint32_t i = n + G::thread(); i < k; i += NT) {
