@@ -146,8 +146,10 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
         else if (words <= 128) run(zero, Shape<64, 2>());
         else if (words <= 512 && k <= 32) run(zero, Shape<64, 8>());
         else if (words <= 1024) run(zero, Shape<256, 4>());
-        else if (words <= 4096 && k <= 64) run(zero, Shape<256, 16>());
+        else if (words <= 2048 && k <= 64) run(zero, Shape<256, 8>());
+        else if (words <= 4096 && k <= 128) run(zero, Shape<512, 8>());
         else if (words <= 4096) run(zero, Shape<1024, 4>());
+        else if (words <= 8192) run(zero, Shape<1024, 8>());
         else run(zero, Shape<1024, 16>());
     });
 }
