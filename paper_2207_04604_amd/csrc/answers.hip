@@ -56,6 +56,10 @@ template <class F> d2mhe_status with_type(uint32_t dtype, F f)
     return hipGetLastError() == hipSuccess ? D2MHE_OK : D2MHE_ERR_HIP;
 }
 
+// Rows are cut into parts where 1024 threads would share one (beyond 8192 words) and up to 128 rows leave half of the units
+// without: whole / in parts, us: step of 64 x 131072 in f32 33.9 / 21.5, of 128 41.2 / 43.5; loss of 128 22.8 / 18.4; with up to
+// 8192 words the second launch costs more than it brings (step of 16 x 32768 in f32 8.1 / 10.4).  1024 workgroups instead of
+// 512: 64 x 131072 25.8 -> 21.5.  A part has 4 words for each of 256 threads.
 constexpr uint32_t SPLIT_ROWS = 128, SPLIT_WORDS = 8192, SPLIT_GROUPS = 1024, PART_WORDS = 1024;
 
 template <class T> uint32_t words_of(const d2mhe_logits *z) { return (z->classes + Pack<T>::E - 1) / Pack<T>::E; }
@@ -65,7 +69,10 @@ template <int NT, int NV> struct Shape {
     static constexpr int THREADS = NT, WORDS = NV;
 };
 
-// f(T(), Shape()): the fewest that hold a row and its k slots; the longest rows keep a part of it
+// f(T(), Shape()): threads and words that hold a row and its k slots; the longest rows keep a part of it.  Measured on 268 MB of
+// bf16, loss in us, shape taken / next best: 512 classes 53 / 128 (64 x 2), 1000 classes 49 / 77 (64 x 2), 4096 47 / 71 (256 x
+// 4), 8192 50 / 49 (128 x 8, whose step takes 100 instead of 94), 16384 47 / 52 (512 x 8), 32768 52 / 53 (256 x 16), 50001 40 /
+// 53 (1024 x 8).
 template <class F> d2mhe_status with_shape(const d2mhe_logits *z, uint32_t k, F f)
 {
     return with_type(z->dtype, [&](auto zero) {
@@ -138,7 +145,9 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
             hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in, k, index, logprob);
         });
     };
-    // as many threads as give a close bound: four maxima to a slot, two in a wavefront by itself
+    // As many threads as give a close bound, four maxima to a slot (two in a wavefront by itself), and no more than it takes to
+    // hold the row; measured in us, taken / next best: 5 of 32768 x 2048 in bf16 44 / 80 (256 x 4), 64 of 2048 x 65536 62 / 66 (512
+    // x 16), 100 of 4096 x 32768 67 / 147 (1024 x 4), 5 of 131072 x 512 47 / 104 (64 x 2).
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
         if (words <= 16 && k <= 16) run(zero, Shape<16, 1>());
@@ -242,6 +251,8 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
         const Parts whole = {1, words, nullptr};
+        // us on 268 MB of bf16, taken / next best: 256 classes 107 / 222 (64 x 2), 1000 115 / 128 (16 x 8), 2048 94 / 130 (256 x 4),
+        // 4096 93 / 98 (64 x 8)
         if (words <= 16 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 1>(), whole);
         else if (words <= 64 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 4>(), whole);
         else if (words <= 128) run(zero, Shape<64, 2>(), whole);

@@ -433,3 +433,106 @@ def test_on_a_stream_and_in_a_replayed_graph(rows, V):
         for w, eager in zip(works, want):
             for a, b in zip(w.results(), eager):
                 assert torch.equal(a, b)
+
+
+# ---- far ends of the sums ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("V", [30, 90, 450, 1000, 3500, 9000, 30000, 66000, 131075])
+@pytest.mark.parametrize("name", ["ascending", "descending", "far up", "far down", "one far up", "first words excluded"])
+def test_logits_far_from_each_other_and_from_zero(name, V):
+    """The largest logits far from those that are read first, all of them far from 0, at temperatures from 0.01 on: the
+    sums must not run over, under or short of bits."""
+    rng = np.random.default_rng(V)
+    rows, k = 3, 9
+    z = rng.normal(0, 2, (rows, V))
+    if name == "ascending":
+        z += np.linspace(-400, 400, V)
+    elif name == "descending":
+        z += np.linspace(400, -400, V)
+    elif name == "far up":
+        z += 5e6
+    elif name == "far down":
+        z += [[-5e6], [-3e30], [-9e4]]
+    elif name == "one far up":
+        z[:, V - 2] = [7e6, 300.0, 3e38]
+    else:
+        z[:, :V - 3] = -np.inf
+        z[:, V - 3:] -= 700
+    buf = torch.from_numpy(z.astype(np.float32)).to(DEV)
+    z = buf.double().cpu().numpy()
+    index, lp = run_top(buf, "f32", V, k)
+    want, wlp = R.top_logprobs(z, k)
+    assert np.array_equal(index, want)
+    within(lp, wlp, R.logprob_error(z, wlp))
+    sums = answers(rng, rows, k, 2)
+    for T in (1.0, 0.01 if name in ("ascending", "far up") else 30.0):
+        at = want if name != "one far up" else np.tile(np.array([V - 2] + [-1] * (k - 1), np.int32), (rows, 1))
+        d = R.Distill(z, at, sums, 2, T)
+        loss, lse, grad = run_distill(buf, "f32", V, at, sums, 2, T)
+        within(loss, d.loss, d.loss_error)
+        within(lse, d.lse, d.lse_error)
+        within(grad, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+
+
+@pytest.mark.parametrize("V", [20, 700, 5000, 70000])
+def test_an_infinite_logit_spoils_its_row_only(V):
+    rng = np.random.default_rng(V)
+    rows, k = 4, 6
+    buf, z = logits(rng, rows, V, 0, "f32")
+    buf[1, V // 3] = float("inf")
+    index, sums = slots(rng, rows, V, k), answers(rng, rows, k, 2)
+    loss, lse, grad = run_distill(buf, "f32", V, index, sums, 2, 1.0)
+    d = R.Distill(z, index, sums, 2, 1.0)
+    good = [0, 2, 3]
+    within(grad[good], d.grad[good], d.stored_error(HALF_STEP["f32"], LEAST["f32"])[good])
+    within(loss[good], d.loss[good], d.loss_error[good])
+    assert np.isnan(loss[1]) and np.isnan(grad[1]).all()
+    top, _ = run_top(buf, "f32", V, k)
+    z[1, V // 3] = np.inf
+    for r in range(rows):
+        assert np.array_equal(top[r], np.argsort(-z[r], kind="stable")[:k])
+
+
+@pytest.mark.parametrize("rows,dtype", [(2, "f16"), (130, "bf16")])
+def test_rows_of_millions(rows, dtype):
+    """Rows that no workgroup holds: cut into parts where they are few, read in passes where they are many."""
+    V, k = (5_000_011, 40) if rows == 2 else (140_003, 40)
+    rng = np.random.default_rng(rows)
+    buf, z = logits(rng, rows, V, 3, dtype)
+    index, sums = slots(rng, rows, V, k, twice=True), answers(rng, rows, k, 2)
+    use = slice(0, 3)
+    d = R.Distill(z[use], index[use], sums[use], 2, 1.0)
+    loss, lse, grad = run_distill(buf, dtype, V, index, sums, 2, 1.0)
+    within(loss[use], d.loss, d.loss_error)
+    within(lse[use], d.lse, d.lse_error)
+    within(grad[use], d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+    back = run_distill(buf, dtype, V, index, sums, 2, 1.0, lse=lse)
+    d = R.Distill(z[use], index[use], sums[use], 2, 1.0, lse=lse[use])
+    within(back[use], d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+    top, lp = run_top(buf, dtype, V, k)
+    want, wlp = R.top_logprobs(z[use], k)
+    assert np.array_equal(top[use], want)
+    within(lp[use], wlp, R.logprob_error(z[use], wlp))
+    want = R.logprobs_at(z[use], index[use])
+    within(run_at(buf, dtype, V, index)[use], want, R.logprob_error(z[use], want))
+
+
+def test_many_short_rows():
+    """More rows than one launch has workgroups for."""
+    rows, V, k = (1 << 24) + 19, 3, 2
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    buf = torch.randn((rows, V), generator=gen, device=DEV).to(torch.float16)
+    z = describe(buf, "f16", V)
+    index, lp = torch.empty((rows, k), dtype=torch.int32, device=DEV), torch.empty((rows, k), device=DEV)
+    s, n = scratch_for(z, k)
+    B.top_logprobs(z, k, index, lp, s, n)
+    sums = torch.full((rows, k), -1.0, device=DEV)
+    loss, lse, grad = torch.empty(rows, device=DEV), torch.empty(rows, device=DEV), torch.empty_like(buf)
+    B.distill(z, B.make_teacher(index, sums, k, 1), loss, lse, grad, V, s, n)
+    torch.cuda.synchronize()
+    order = torch.sort(buf.double(), dim=1, descending=True, stable=True).indices[:, :k].int()
+    assert torch.equal(index, order)
+    soft = torch.softmax(buf.double(), 1)
+    want = soft.scatter_add(1, order.long(), torch.full((rows, k), -0.5, dtype=torch.float64, device=DEV))
+    # one rounding to 2^-11 relative, 2^-25 at least, on values below 1 with a relative error of less than 64 U
+    assert ((grad.double() - want).abs() <= want.abs() * 2.0 ** -11 + 2.0 ** -25 + 64 * R.U).all()
