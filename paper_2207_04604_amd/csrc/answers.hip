@@ -70,9 +70,8 @@ template <int NT, int NV> struct Shape {
 };
 
 // f(T(), Shape()): threads and words that hold a row and its k slots; the longest rows keep a part of it.  Measured on 268 MB of
-// bf16, loss in us, shape taken / next best: 512 classes 53 / 128 (64 x 2), 1000 classes 49 / 77 (64 x 2), 4096 47 / 71 (256 x
-// 4), 8192 50 / 49 (128 x 8, whose step takes 100 instead of 94), 16384 47 / 52 (512 x 8), 32768 52 / 53 (256 x 16), 50001 40 /
-// 53 (1024 x 8).
+// bf16, us, shape taken / next best: loss of 512 classes 53 / 127 (64 x 2), 1000 49 / 77 (64 x 2), 4096 47 / 71 (256 x 4), 16384
+// 47 / 52 (512 x 8); step of 8192 94 / 100 (128 x 8), 32768 55 / 57 (256 x 16); loss of 777 x 50001 in f16 19 / 25 (1024 x 8).
 template <class F> d2mhe_status with_shape(const d2mhe_logits *z, uint32_t k, F f)
 {
     return with_type(z->dtype, [&](auto zero) {
@@ -251,7 +250,7 @@ d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);
         const Parts whole = {1, words, nullptr};
-        // us on 268 MB of bf16, taken / next best: 256 classes 107 / 222 (64 x 2), 1000 115 / 128 (16 x 8), 2048 94 / 130 (256 x 4),
+        // us on 268 MB of bf16, taken / next best: 256 classes 107 / 222 (64 x 2), 700 115 / 128 (16 x 8), 2048 94 / 130 (256 x 4),
         // 4096 93 / 98 (64 x 8)
         if (words <= 16 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 1>(), whole);
         else if (words <= 64 && teacher->k <= Group<16>::TOP) run(zero, Shape<16, 4>(), whole);

@@ -599,8 +599,8 @@ template <class T, int NT, int NV, int BITS, class R, class Key> __device__ uint
 // Two rounds over a row in registers.  The first gives the maximum of every thread; the `each`-th largest of a wavefront's
 // maxima, the least of them over the wavefronts, is a bound that at least k elements reach.  (Few words or many slots: the
 // bound comes from the elements themselves.)  The second collects what reaches it, usually little more than k, in LDS, where
-// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 247 us, 4.3 TB/s, of which 205 us
-// are the reading; vector ALU three quarters busy.  5 of 65536 x 100 in f16: 12 us, bound by its instructions.  (Four lanes
+// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 247 us, 4.3 TB/s (185
+// without the second round); vector ALU three quarters busy.  5 of 65536 x 100 in f16: 12 us, bound by its instructions.  (Four lanes
 // to a candidate: 264 us; the next row's words requested as this row's are looked through: 302, the compiler keeps both.)
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, int32_t *index, float *out)
