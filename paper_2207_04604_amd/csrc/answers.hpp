@@ -40,9 +40,9 @@ __device__ inline float neg_inf() { return -__builtin_inff(); }
 
 // ---- 16 bytes of logits -----------------------------------------------------------------------------------
 
-typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
+typedef uint32_t Word4 __attribute__((ext_vector_type(4), may_alias));
 // any alignment of an element: the machine takes 16-byte accesses at odd addresses
-typedef Word4 Word4Any __attribute__((aligned(2)));
+typedef Word4 Word4Any __attribute__((aligned(2), may_alias));
 
 template <class T> struct Pack;                 // E elements in 16 bytes
 template <> struct Pack<float> {
@@ -469,9 +469,6 @@ template <class T> struct Keys<T, uint32_t> {
     }
     static __device__ int32_t position(uint32_t k) { return (int32_t)(0xffffu - (k & 0xffffu)); }
 };
-template <class K> struct alignas(16) Four {
-    K k[16 / sizeof(K)];
-};
 
 // A number t that at least `count` of the keys reach, and none but equal ones more, among the keys of the group's lanes of a
 // wavefront (N keys to a lane); 0 if there are not as many keys above 0.  Bit by bit from the top, of the given leading bits.
@@ -599,9 +596,9 @@ template <class T, int NT, int NV, int BITS, class R, class Key> __device__ uint
 // Two rounds over a row in registers.  The first gives the maximum of every thread; the `each`-th largest of a wavefront's
 // maxima, the least of them over the wavefronts, is a bound that at least k elements reach.  (Few words or many slots: the
 // bound comes from the elements themselves.)  The second collects what reaches it, usually little more than k, in LDS, where
-// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 247 us, 4.3 TB/s (185
-// without the second round); vector ALU three quarters busy.  5 of 65536 x 100 in f16: 12 us, bound by its instructions.  (Four lanes
-// to a candidate: 264 us; the next row's words requested as this row's are looked through: 302, the compiler keeps both.)
+// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 247 us, 4.3 TB/s (185 without the
+// second round); vector ALU three quarters busy.  5 of 65536 x 100 in f16: 12 us, bound by its instructions.  (Four lanes to a
+// candidate: 261 us; the next row's words requested as this row's are looked through: 302, the compiler keeps both.)
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, int32_t *index, float *out)
 {
