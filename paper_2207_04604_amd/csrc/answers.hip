@@ -141,11 +141,14 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
         using T = decltype(zero);
         constexpr int NT = decltype(shape)::THREADS, NV = decltype(shape)::WORDS;
         each_launch<NT>(z, [&](dim3 grid, Rows in) {
-            hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in, k, index, logprob);
+            if constexpr (NT >= 512)
+                hipLaunchKernelGGL((k_top_long<T, NT, NV>), grid, dim3(NT), 0, (hipStream_t)stream, in, k, index, logprob);
+            else
+                hipLaunchKernelGGL((k_top<T, NT, NV>), grid, dim3(Group<NT>::SIZE), 0, (hipStream_t)stream, in, k, index, logprob);
         });
     };
     // As many threads as give a close bound, four maxima to a slot (two in a wavefront by itself), and no more than it takes to
-    // hold the row; measured in us, taken / next best: 5 of 32768 x 2048 in bf16 44 / 80 (256 x 4), 64 of 2048 x 65536 62 / 66 (512
+    // hold the row; measured in us, taken / next best: 5 of 32768 x 2048 in bf16 44 / 80 (256 x 4), 64 of 2048 x 65536 64 / 66 (512
     // x 16), 100 of 4096 x 32768 67 / 147 (1024 x 4), 5 of 131072 x 512 47 / 104 (64 x 2).
     return with_type(z->dtype, [&](auto zero) {
         const uint32_t words = words_of<decltype(zero)>(z);

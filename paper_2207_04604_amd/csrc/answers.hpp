@@ -497,8 +497,57 @@ template <> struct OrderBits<_Float16> { static constexpr int N = 19; };
 
 constexpr uint32_t CANDIDATES = 1024;
 
+// The keys of a row's elements that equal `value`, from the lowest position on, to best[have] and on until there are k; returns
+// how many there are then.  One turn of the threads after the other, the elements before the words first and those behind
+// them last: most rows of many equal values end with the first words.
+template <class T, int NT, class R, class Key> __device__ uint32_t equal_in_order(const R &row, float value, uint32_t have, uint32_t k, Key *best)
+{
+    using P = Pack<T>;
+    __shared__ uint32_t totals[Group<NT>::WAVES];
+    const uint32_t turns = (row.n + NT - 1) / NT;
+#pragma unroll 1
+    for (uint32_t turn = 0; turn < turns + 2 && have < k; ++turn) {
+        float x[P::E];
+        uint32_t at = 0, equal = 0;
+#pragma unroll
+        for (int e = 0; e < P::E; ++e) x[e] = neg_inf();
+        if (turn == 0 || turn == turns + 1) {
+            if (row.at != 0xffffffffu && (row.at < row.head) == (turn == 0)) {
+                at = row.at;
+                x[0] = row.edge;
+            }
+        } else {
+            const uint32_t c = (turn - 1) * NT + threadIdx.x;
+            at = row.head + c * P::E;
+            if (c < row.n) P::open(row.words[c], x);
+        }
+#pragma unroll
+        for (int e = 0; e < P::E; ++e) equal += x[e] == value;
+        uint32_t before = equal;
+        for (int d = 1; d < 64; d *= 2) {
+            const uint32_t other = __shfl_up(before, d);
+            if ((int)(threadIdx.x & 63) >= d) before += other;
+        }
+        if ((threadIdx.x & 63) == 63) totals[threadIdx.x >> 6] = before;
+        __syncthreads();
+        uint32_t all = 0;
+        before -= equal;
+        for (uint32_t w = 0; w < Group<NT>::WAVES; ++w) {
+            if (w < threadIdx.x >> 6) before += totals[w];
+            all += totals[w];
+        }
+        before += have;
+#pragma unroll
+        for (int e = 0; e < P::E; ++e)
+            if (x[e] == value && before < k) best[before++] = Keys<T, Key>::of(x[e], at + e);
+        have += all;
+        __syncthreads();
+    }
+    return have < k ? have : k;
+}
+
 // The k-th largest key digit by digit from the top: the counts of the next eight bits among the keys that agree with the
-// digits chosen so far. For rows with more candidates than LDS has room for, such as many equal values.
+// digits chosen so far. For rows with more candidates than LDS has room for.
 template <class T, int NT, class R> __device__ uint64_t least_by_digits(R &row, uint32_t k, uint32_t *count)
 {
     __shared__ uint64_t least;
@@ -539,7 +588,7 @@ template <class T, int NT, class R> __device__ uint64_t least_by_digits(R &row, 
 template <class T, int NT, int NV, int BITS, class R, class Key> __device__ uint32_t best_of_many(R &row, uint32_t k, Key *best)
 {
     using P = Pack<T>;
-    constexpr uint32_t MASK = BITS == 32 ? 0xffffffffu : ~(0xffffffffu >> BITS);
+    constexpr uint32_t MASK = ~(uint32_t)(0xffffffffull >> BITS);
     auto count = [&](auto f) {
         uint32_t n = 0;
         row.each([&](Word4 w) {
@@ -596,11 +645,10 @@ template <class T, int NT, int NV, int BITS, class R, class Key> __device__ uint
 // Two rounds over a row in registers.  The first gives the maximum of every thread; the `each`-th largest of a wavefront's
 // maxima, the least of them over the wavefronts, is a bound that at least k elements reach.  (Few words or many slots: the
 // bound comes from the elements themselves.)  The second collects what reaches it, usually little more than k, in LDS, where
-// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 247 us, 4.3 TB/s (185 without the
+// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 250 us, 4.3 TB/s (185 without the
 // second round); vector ALU three quarters busy.  5 of 65536 x 100 in f16: 12 us, bound by its instructions.  (Four lanes to a
 // candidate: 261 us; the next row's words requested as this row's are looked through: 302, the compiler keeps both.)
-template <class T, int NT, int NV>
-__global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, int32_t *index, float *out)
+template <class T, int NT, int NV> __device__ __forceinline__ void top_of_row(const Rows &in, uint32_t k, int32_t *index, float *out)
 {
     using G = Group<NT>;
     using P = Pack<T>;
@@ -730,6 +778,22 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         if (n > ROOM) n = best_of_many<T, NT, NV, BITS>(row, k, best[group]);
     }
     if (NT > 64 && n > ROOM) {
+        // Many equal to the bound, as in a row of few values (4096 x 131072 zeros in bf16: 458 us; by digits: 13009)?  What
+        // exceeds it, and of the equal ones the first.
+        __syncthreads();
+        if (threadIdx.x == 0) found[0] = 0;
+        __syncthreads();
+        row.elements_again([&](float x, uint32_t v) {
+            if (x > least) {
+                const uint32_t i = atomicAdd(&found[0], 1u);
+                if (i < ROOM) best[0][i] = K::of(x, v);
+            }
+        });
+        __syncthreads();
+        n = found[0];
+        if (n < k) n = equal_in_order<T, NT>(row, least, n, k, best[0]);
+    }
+    if (NT > 64 && n > ROOM) {
         __shared__ uint32_t count[256];
         const uint64_t last = least_by_digits<T, NT>(row, k, count);
         if (threadIdx.x == 0) found[0] = 0;
@@ -762,6 +826,20 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
         index[r * k + i] = -1;
         out[r * k + i] = 0;
     }
+}
+
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, int32_t *index, float *out)
+{
+    top_of_row<T, NT, NV>(in, k, index, out);
+}
+
+// 512 and 1024 threads, as many such workgroups to a unit as make eight wavefronts a SIMD: that leaves each no more than 80 of
+// the scalar registers that the compiler may give it (64 of 2048 x 65536 in bf16 with 93 of them: 84 us instead of 64).
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(NT) __attribute__((amdgpu_num_sgpr(80))) k_top_long(Rows in, uint32_t k, int32_t *index, float *out)
+{
+    top_of_row<T, NT, NV>(in, k, index, out);
 }
 
 // ---- distillation ----------------------------------------------------------------------------------------

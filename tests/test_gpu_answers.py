@@ -536,3 +536,25 @@ def test_many_short_rows():
     want = soft.scatter_add(1, order.long(), torch.full((rows, k), -0.5, dtype=torch.float64, device=DEV))
     # one rounding to 2^-11 relative, 2^-25 at least, on values below 1 with a relative error of less than 64 U
     assert ((grad.double() - want).abs() <= want.abs() * 2.0 ** -11 + 2.0 ** -25 + 64 * R.U).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,pad,k", [(3001, 1, 70), (9001, 3, 256), (20003, 5, 100), (70001, 0, 33), (140001, 2, 256)])
+def test_many_equal_and_few_larger(V, pad, k, dtype):
+    """More equal values at the border than there is room for, also at the ends of rows at odd addresses."""
+    rng = np.random.default_rng(V)
+    z = np.zeros((7, V), np.float32)
+    z[1, rng.permutation(V)[:10]] = 1 + rng.integers(0, 100, 10)
+    z[2, :V // 2] = -1
+    z[3, rng.permutation(V)[:k + 44]] = 2
+    z[4, 5:V - 3] = -2                                              # all of the largest are at the ends
+    z[6, ::3] = -0.0
+    z[6, 1::7] = 0.5
+    buf = torch.full((7, V + pad), float("nan"), dtype=TORCH[dtype], device=DEV)
+    buf[:, :V] = torch.from_numpy(z).to(TORCH[dtype]).to(DEV)
+    buf[5, :V] = torch.finfo(TORCH[dtype]).min
+    z = buf[:, :V].double().cpu().numpy()
+    index, lp = run_top(buf, dtype, V, k)
+    want, wlp = R.top_logprobs(z, k)
+    assert np.array_equal(index, want)
+    within(lp, wlp, R.logprob_error(z, wlp))
