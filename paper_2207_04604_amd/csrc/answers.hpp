@@ -367,7 +367,7 @@ template <class T, int NT, int NV> struct Row {
         }
         return {m, across<Add, G::LANES>(s)};
     }
-    // grad = f * exp2((x - m) * scale)
+    // grad = f * exp2((x - m) * scale), rounded to nearest once, here; exp2 of the machine is 0 below 2^-126
     __device__ void store(T *out, float m, float scale, float f)
     {
         const float top = m * scale;
