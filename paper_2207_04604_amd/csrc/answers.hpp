@@ -110,7 +110,8 @@ template <> struct Pack<_Float16> {
     static constexpr uint32_t NONE = 0xfc00fc00u;
 };
 
-// fmaxf without the quieting of signalling NaNs that it costs on values that come straight from memory
+// fmaxf without the quieting of signalling NaNs that it costs on values that come straight from memory: where one of them is a
+// signalling NaN, the others may get lost
 __device__ inline float max3(float a, float b, float c)
 {
     float r;
@@ -710,11 +711,13 @@ template <class T, int NT, int NV> __device__ __forceinline__ void top_of_row(co
         }
     };
     if (NT != 16 && row.at != 0xffffffffu) keep(row.edge, row.at);
+    // A row with a NaN has a sum of NaN: there every word reaches, as max3 may lose what stands next to a signalling one.
+    const float border = st.s == st.s ? least : neg_inf();
     auto reaches = [&](const float *x) {
         float most = x[0];
 #pragma unroll
         for (int i = 1; i + 1 < P::E; i += 2) most = max3(most, x[i], x[i + 1]);
-        return max3(most, x[P::E - 1], most) >= least;
+        return !(max3(most, x[P::E - 1], most) < border);
     };
     uint32_t taken = 0;
     if constexpr (NT == 16) {

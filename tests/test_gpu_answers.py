@@ -558,3 +558,32 @@ def test_many_equal_and_few_larger(V, pad, k, dtype):
     want, wlp = R.top_logprobs(z, k)
     assert np.array_equal(index, want)
     within(lp, wlp, R.logprob_error(z, wlp))
+
+
+# ---- values that a comparison may lose --------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V,pad,k", [(104, 0, 5), (600, 0, 20), (600, 3, 20), (1000, 0, 100), (3000, 1, 20), (5000, 0, 30), (12000, 0, 200), (70000, 0, 64),
+                                     (140008, 5, 64)])
+def test_signalling_nans_beside_the_largest(V, pad, k, dtype):
+    """A NaN is never chosen and hides none of its neighbours, whether it is a quiet or a signalling one."""
+    rng = np.random.default_rng(V + pad)
+    rows, whole = 5, {"f32": np.int32, "bf16": np.int16}[dtype]
+    value = rng.normal(0, 1, (rows, V))
+    nan = np.zeros((rows, V), bool)
+    for r in range(rows):
+        large = rng.permutation(V)[:k]
+        value[r, large] = 20 + rng.permutation(k) / 8
+        beside = (large[:, None] + np.arange(-3, 4)[None]).clip(0, V - 1)
+        nan[r, beside[rng.random(beside.shape) < 0.4]] = True
+        nan[r, large] = False
+    z = torch.from_numpy(value.astype(np.float32)).to(TORCH[dtype])
+    least = {"f32": 0x7f800001, "bf16": 0x7f81}[dtype]                # of the signalling NaNs, and with a sign
+    bits = z.view(torch.int32 if dtype == "f32" else torch.int16).numpy()
+    bits[nan] = np.where(rng.random(nan.sum()) < 0.5, least, least - (1 << 8 * bits.itemsize - 1)).astype(whole)
+    buf = torch.zeros((rows, V + pad), dtype=TORCH[dtype], device=DEV)
+    buf[:, :V] = z.to(DEV)
+    index, lp = run_top(buf, dtype, V, k)
+    want, _ = R.top_logprobs(np.where(nan, np.nan, z.double().numpy()), k)
+    assert np.array_equal(index, want)
+    assert np.isnan(lp[nan.any(1)]).all()
