@@ -472,7 +472,8 @@ template <class T> struct Keys<T, uint32_t> {
 };
 
 // A number t that at least `count` of the keys reach, and none but equal ones more, among the keys of the group's lanes of a
-// wavefront (N keys to a lane); 0 if there are not as many keys above 0.  Bit by bit from the top, of the given leading bits.
+// wavefront (N keys to a lane); 0 if there are not as many keys above 0.  Bit by bit from the top, of the given leading bits:
+// the bits below are 0, also where those of a negative value are ones.
 template <int NT, int BITS, int N> __device__ inline uint32_t nth_largest(const uint32_t *keys, uint32_t count)
 {
     uint32_t t = 0;
@@ -703,7 +704,7 @@ template <class T, int NT, int NV> __device__ __forceinline__ void top_of_row(co
     }
     const float log_s = __logf(st.s), m = st.m;
     // the least finite value leaves out -inf and NaN
-    const float least = bound ? value_of(bound) : -3.402823466e38f;
+    float least = bound ? value_of(bound) : -3.402823466e38f;
     auto keep = [&](float x, uint32_t v) {
         if (x >= least) {
             const uint32_t i = atomicAdd(&found[group], 1u);
@@ -781,10 +782,34 @@ template <class T, int NT, int NV> __device__ __forceinline__ void top_of_row(co
         if (n > ROOM) n = best_of_many<T, NT, NV, BITS>(row, k, best[group]);
     }
     if (NT > 64 && n > ROOM) {
-        // Many equal to the bound, as in a row of few values (4096 x 131072 zeros in bf16: 458 us; by digits: 13009)?  What
-        // exceeds it, and of the equal ones the first.
+        // Many equal to the bound, as in a row of few values (1024 x 131072 in bf16, zeros 123 us, -7 123; by digits 3240)?  What
+        // exceeds it, and of the equal ones the first.  The bound has to be a value of the row for that: it lies below those that
+        // it was made from where they are negative and of 16 bits, or where the search for it ended early.
         __syncthreads();
         if (threadIdx.x == 0) found[0] = 0;
+        if (bound) {
+            uint32_t low = 0xffffffffu;
+            const auto lower = [&](float x) {
+                if (order_of(x) >= bound) low = Min::of(low, order_of(x));
+            };
+            if constexpr (NV <= 4) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    float x[P::E];
+                    P::open(row.fresh(i), x);
+#pragma unroll
+                    for (int e = 0; e < P::E; ++e) lower(x[e]);
+                }
+                lower(row.edge);
+            } else {
+                lower(mine);
+            }
+            low = across<Min, 64>(low);
+            if ((threadIdx.x & 63) == 0) bounds[G::wave()] = low;
+            __syncthreads();
+            for (int i = 0; i < G::WAVES; ++i) low = Min::of(low, bounds[i]);
+            least = value_of(low);
+        }
         __syncthreads();
         row.elements_again([&](float x, uint32_t v) {
             if (x > least) {
