@@ -44,7 +44,7 @@ Rows rows_of(const d2mhe_logits *z) { return {z->logits, z->row_stride, 0, z->ro
 
 Answers answers_of(const d2mhe_teacher *t)
 {
-    return {t->index, t->sum, t->weight, t->k, 1.0f / (float)t->members, 1.0f / t->temperature};
+    return {t->index, t->sum, t->weight, t->k, (float)(1.0 / ((double)t->members * t->temperature)), 1.0f / t->temperature};
 }
 
 // f(T()) with the element type of the logits

@@ -29,7 +29,7 @@ struct Answers {
     const int32_t *index;
     const float *sum, *weight;
     uint32_t k;
-    float inv_members, inv_t;
+    float share, inv_t;                 // a sum's factor to s / T: 1 / (members * T); 1 / T
 };
 
 __device__ inline float to_float(float x) { return x; }
@@ -890,8 +890,9 @@ template <int NT> struct Taught {
     }
 };
 
-// The teacher's slots j of a row, slot j with thread j % NT: class (-1: empty) and answer t = s_j / T, and their softmax:
-// u = exp(t - m) for the largest t of the wavefront, later of the row.
+// The teacher's slots j of a row, slot j with thread j % NT: class (-1: empty) and sum of answers t, and their softmax:
+// u = exp((t - m) * share) for the largest t of the wavefront, later of the row.  The difference comes before the product: a sum
+// by itself, lowest values among them, may leave the range when it is divided by a temperature below 1.
 template <int NT> struct Slots {
     using G = Group<NT>;
     int32_t v[G::SLOTS];
@@ -911,7 +912,7 @@ template <int NT> struct Slots {
                 const float s = a.sum[r * a.k + j];
                 if ((uint32_t)c < classes && s != neg_inf()) {
                     v[i] = c;
-                    t[i] = s * a.inv_members * a.inv_t;
+                    t[i] = s;
                 }
             }
             own[i] = v[i] >= 0;
@@ -920,7 +921,7 @@ template <int NT> struct Slots {
     // u and its sum within the wavefront; and whether a class comes twice: of two slots of a class one finds the other in a
     // table of twice as many places as slots.  (All slots going through all others: 90 us instead of 63 for gradients of
     // 512 x 65537 with 250 slots, 527 instead of 471 for a step of 4096 x 131072 with 128.)
-    __device__ void weigh(Taught<NT> &lds, uint32_t group)
+    __device__ void weigh(float share, Taught<NT> &lds, uint32_t group)
     {
         float m = neg_inf(), sum = 0;
 #pragma unroll
@@ -930,7 +931,7 @@ template <int NT> struct Slots {
         for (int i = 0; i < G::SLOTS; ++i) {
             u[i] = 0;
             if (v[i] < 0) continue;
-            u[i] = __builtin_amdgcn_exp2f((t[i] - m) * LOG2E);
+            u[i] = __builtin_amdgcn_exp2f((t[i] - m) * (share * LOG2E));
             sum += u[i];
             if (!own[i]) continue;
             constexpr uint32_t LAST = Taught<NT>::PLACES - 1;
@@ -946,10 +947,10 @@ template <int NT> struct Slots {
         G::put(st, lds.stats);
     }
     // After a barrier: u and its sum for the row.
-    __device__ void join(uint32_t k, Taught<NT> &lds, uint32_t group)
+    __device__ void join(uint32_t k, float share, Taught<NT> &lds, uint32_t group)
     {
-        const Stats all = G::get(st, lds.stats, LOG2E);
-        const float f = all.m == st.m ? 1.0f : __builtin_amdgcn_exp2f((st.m - all.m) * LOG2E);
+        const Stats all = G::get(st, lds.stats, share * LOG2E);
+        const float f = all.m == st.m ? 1.0f : __builtin_amdgcn_exp2f((st.m - all.m) * (share * LOG2E));
         st = all;
 #pragma unroll
         for (int i = 0; i < G::SLOTS; ++i) {
@@ -961,14 +962,14 @@ template <int NT> struct Slots {
             }
         }
     }
-    // sum_j p_j (log p_j - (z_j / T - lse)) = A / U - log U + log S with the sum A of u_j (t_j - m - (z_j - m_z) / T); A by
-    // wavefronts
-    __device__ void part_of_loss(const float *x, Stats z, float inv_t, Taught<NT> &lds)
+    // sum_j p_j (log p_j - (z_j / T - lse)) = A / U - log U + log S with the sum A of u_j ((t_j - m) * share - (z_j - m_z) / T); A
+    // by wavefronts
+    __device__ void part_of_loss(const float *x, Stats z, const Answers &a, Taught<NT> &lds)
     {
         float sum = 0;
 #pragma unroll
         for (int i = 0; i < G::SLOTS; ++i)
-            if (u[i] != 0.0f) sum += u[i] * ((t[i] - st.m) - (x[i] - z.m) * inv_t);
+            if (u[i] != 0.0f) sum += u[i] * ((t[i] - st.m) * a.share - (x[i] - z.m) * a.inv_t);
         sum = across<Add, G::LANES>(sum);
         if (NT <= 64) st.m = sum;
         else if ((threadIdx.x & 63) == 0) lds.loss[G::wave()] = sum;
@@ -1024,12 +1025,12 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
     for (int i = 0; i < G::SLOTS; ++i) x[i] = slots.v[i] >= 0 ? to_float(row.z[slots.v[i]]) : 0.0f;
     taught.clear(group);
     G::sync();
-    slots.weigh(taught, group);
+    slots.weigh(a.share, taught, group);
     Stats st = row.stats(scale, mine);
     G::put(st, buf);
     G::sync();
     st = G::get(st, buf, scale);
-    slots.join(a.k, taught, group);
+    slots.join(a.k, a.share, taught, group);
     // neither a weight nor a filled slot, or all logits -inf
     const bool none = w == 0.0f || slots.st.s == 0.0f, excluded = !none && st.s == 0.0f;
     if (none || excluded) {
@@ -1041,7 +1042,7 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_distill(Rows in, Answers a,
         return;
     }
     const float g = w * a.inv_t, gs = g / st.s, gu = g / slots.st.s;
-    slots.part_of_loss(x, st, a.inv_t, taught);
+    slots.part_of_loss(x, st, a, taught);
     if (GRAD) row.store(out, st.m, scale, gs);
     G::sync();
     if (G::thread() == 0) {
@@ -1126,14 +1127,14 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     }
     taught.clear(group);
     G::sync();
-    slots.weigh(taught, group);
+    slots.weigh(a.share, taught, group);
     if (SPLIT) {
         st = st.together<G::LANES>(scale);
         G::put(st, buf);
     }
     G::sync();
     if (SPLIT) st = G::get(st, buf, scale);
-    slots.join(a.k, taught, group);
+    slots.join(a.k, a.share, taught, group);
     const bool none = w == 0.0f || slots.st.s == 0.0f, excluded = SPLIT ? !none && st.s == 0.0f : l == neg_inf();
     if (none || excluded) {
         if (SPLIT && part == 0 && threadIdx.x == 0) {
@@ -1148,7 +1149,7 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     auto student = [&](float z) {
         return __builtin_amdgcn_exp2f(SPLIT ? (z - st.m) * scale : __builtin_fmaf(z, a.inv_t, -l) * LOG2E) * gs;
     };
-    if (SPLIT && part == 0) slots.part_of_loss(x, st, a.inv_t, taught);
+    if (SPLIT && part == 0) slots.part_of_loss(x, st, a, taught);
     if (GRAD) {
         row.each_at([&](Word4 words, uint32_t v) {
             float y[P::E];

@@ -630,3 +630,32 @@ def test_equal_values_of_any_sign_take_as_long(name, dtype):
     if name != "the lowest value":
         within(lp[:2].cpu().numpy(), wlp, R.logprob_error(z64, wlp))
     assert other <= 4 * zeros, (other, zeros)
+
+
+@pytest.mark.parametrize("V,k", [(40, 11), (2000, 20), (70001, 200), (300000, 100)])
+def test_teacher_sums_at_the_ends_of_their_range(V, k):
+    """Sums that leave the range of 32 bits when they are divided by a temperature below 1: what counts is how far they are from
+    the largest of their row.  Those equal to it share the mass: p = 1 / their number, with the roundings of their sum, its
+    reciprocal and two products; the student's part as everywhere."""
+    rng = np.random.default_rng(V)
+    rows, T, low = 5, 0.25, np.finfo(np.float32).min
+    buf, z = logits(rng, rows, V, 0, "f32")
+    index, sums = slots(rng, rows, V, k), np.zeros((rows, k), np.float32)
+    share = np.ones((rows, k))
+    sums[0] = low                                                   # a mask that leaves nothing
+    sums[1] = 3e38
+    sums[2, 1:] = low
+    sums[3] = -2e38
+    sums[3, ::2] = -3e38
+    sums[4, 1::2] = -1e38                                           # the largest within the range, the others not
+    share[2, 1:] = share[3, ::2] = share[4, 1::2] = 0
+    share /= share.sum(1, keepdims=True)
+    even = np.where(share > 0, 0.0, -30.0).astype(np.float32)       # the same softmax (exp(-120) is nothing here), for the oracle
+    d = R.Distill(z, index, even, 1, T)
+    loss, lse, grad = run_distill(buf, "f32", V, index, sums, 1, T)
+    within(grad, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+    within(lse, d.lse, d.lse_error)
+    within(loss, d.loss, d.loss_error)
+    back = run_distill(buf, "f32", V, index, sums, 1, T, lse=lse)
+    d = R.Distill(z, index, even, 1, T, lse=lse)
+    within(back, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
