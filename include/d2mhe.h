@@ -319,7 +319,8 @@ d2mhe_status d2mhe_distill(const d2mhe_logits *z, const d2mhe_teacher *teacher, 
  * temperature (a loss whose gradient turns out to be needed later).  A weight other than the one of
  * the loss is the place for the gradient that arrives at it; rows of weight 0 there have no lse and need
  * weight 0 here.  exp(z_v / T - lse) carries lse's rounding: a relative error of up to 2^-24 |lse|.
- * Rows with lse -inf give 0.                                                                        */
+ * Rows whose |lse| is 32768 or more (nothing but lowest values, logits far from 0 at a low temperature)
+ * are summed up again from their logits, without that error.  Rows whose logits are all -inf give 0. */
 d2mhe_status d2mhe_distill_backward(const d2mhe_logits *z, const d2mhe_teacher *teacher, const float *lse,
                                     void *grad, uint64_t grad_stride, void *stream);
 

@@ -1087,6 +1087,28 @@ __device__ inline Stats load_parts(const Parts &parts, uint64_t r)
     return threadIdx.x < parts.count ? parts.stats[r * parts.count + threadIdx.x] : Stats{neg_inf(), 0.0f};
 }
 
+// An lse from here on has a rounding of 2^-9 or more: exp(z / T - lse) would be off by as much, and by a factor of the number of
+// classes in a row of nothing but the lowest value of 32 bits, whose lse has no bits left for log V.
+constexpr float FAR_LSE = 32768.0f;
+
+// Statistics of a whole row, read from memory by its group of threads, once per part: for what hardly ever runs (512 x 65537 in
+// f32, 17 parts to a row, 804 us where all rows are such, 63 where none is).
+template <class T, int NT> __device__ Stats stats_again(const T *z, uint32_t classes, float scale, Stats *buf)
+{
+    using G = Group<NT>;
+    float m = neg_inf(), s = 0;
+#pragma unroll 1
+    for (uint32_t v = G::thread(); v < classes; v += NT) m = fmaxf(m, to_float(z[v]));
+    m = across<Max, G::LANES>(m);
+    if (m != neg_inf())
+#pragma unroll 1
+        for (uint32_t v = G::thread(); v < classes; v += NT) s += __builtin_amdgcn_exp2f((to_float(z[v]) - m) * scale);
+    const Stats st = {m, across<Add, G::LANES>(s)};
+    G::put(st, buf);
+    G::sync();
+    return G::get(st, buf, scale);
+}
+
 // The gradient of a part of a row, or with NT < 256 of a whole one, from its statistics: the lse of an earlier call, or with
 // SPLIT the sums of its parts, where part 0 writes loss and lse as well.  Every part weighs the teacher's slots by itself, and
 // fetches and stores those whose class it has (all parts fetching all: 63.8 us instead of 55 for 512 x 65537 in f32 with 250
@@ -1135,8 +1157,9 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     G::sync();
     if (SPLIT) st = G::get(st, buf, scale);
     slots.join(a.k, a.share, taught, group);
-    const bool none = w == 0.0f || slots.st.s == 0.0f, excluded = SPLIT ? !none && st.s == 0.0f : l == neg_inf();
-    if (none || excluded) {
+    const bool none = w == 0.0f || slots.st.s == 0.0f, far = !SPLIT && !none && fabsf(l) >= FAR_LSE;
+    if (far) st = stats_again<T, NT>(z, in.classes, scale, buf);
+    if (none || st.s == 0.0f) {
         if (SPLIT && part == 0 && threadIdx.x == 0) {
             loss[r] = 0;
             lse[r] = none ? 0.0f : neg_inf();
@@ -1146,19 +1169,21 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     }
     const float g = w * a.inv_t, gs = g / st.s, gu = g / slots.st.s;
     // z / T is not rounded before lse is taken off
-    auto student = [&](float z) {
-        return __builtin_amdgcn_exp2f(SPLIT ? (z - st.m) * scale : __builtin_fmaf(z, a.inv_t, -l) * LOG2E) * gs;
+    auto student = [&](float z, bool by_stats) {
+        return __builtin_amdgcn_exp2f(by_stats ? (z - st.m) * scale : __builtin_fmaf(z, a.inv_t, -l) * LOG2E) * gs;
     };
     if (SPLIT && part == 0) slots.part_of_loss(x, st, a, taught);
     if (GRAD) {
-        row.each_at([&](Word4 words, uint32_t v) {
+        auto store = [&](Word4 words, uint32_t v, bool by_stats) {
             float y[P::E];
             P::open(words, y);
 #pragma unroll
-            for (int i = 0; i < P::E; ++i) y[i] = student(y[i]);
+            for (int i = 0; i < P::E; ++i) y[i] = student(y[i], by_stats);
             *(Word4Any *)(out + v) = P::close(y);
-        });
-        if (row.at != 0xffffffffu) out[row.at] = (T)student(row.edge);
+        };
+        if (far) row.again_at([&](Word4 words, uint32_t v) { store(words, v, true); });
+        else row.each_at([&](Word4 words, uint32_t v) { store(words, v, SPLIT); });
+        if (row.at != 0xffffffffu) out[row.at] = (T)student(row.edge, SPLIT || far);
     }
     G::sync();
     if (SPLIT && part == 0 && threadIdx.x == 0) {
@@ -1168,7 +1193,7 @@ k_gradient(Rows in, Answers a, Parts parts, float *loss, float *lse, T *grad, ui
     if (!GRAD) return;
 #pragma unroll
     for (int i = 0; i < G::SLOTS; ++i)
-        if (slots.own[i]) out[slots.v[i]] = (T)(student(x[i]) - slots.of_class(i, a.k, taught, group) * gu);
+        if (slots.own[i]) out[slots.v[i]] = (T)(student(x[i], SPLIT || far) - slots.of_class(i, a.k, taught, group) * gu);
 }
 
 // Log-probabilities of rows whose parts have been summed up.

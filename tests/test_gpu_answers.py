@@ -659,3 +659,35 @@ def test_teacher_sums_at_the_ends_of_their_range(V, k):
     back = run_distill(buf, "f32", V, index, sums, 1, T, lse=lse)
     d = R.Distill(z, index, even, 1, T, lse=lse)
     within(back, d.grad, d.stored_error(HALF_STEP["f32"], LEAST["f32"]))
+
+
+@pytest.mark.parametrize("dtype", list(TORCH))
+@pytest.mark.parametrize("V", [10, 101, 300, 900, 2001, 9000, 40003])
+@pytest.mark.parametrize("T", [0.25, 1.0, 8.0])
+def test_gradient_alone_of_rows_far_from_zero(T, V, dtype):
+    """Rows whose lse is so far from 0 that it has lost the logarithm of the sum, or is beyond 32 bits: nothing but the type's
+    lowest value, or all logits far up or down.  The gradient alone is that of the pass with the loss."""
+    rng = np.random.default_rng(V)
+    far = {"f32": 5e6, "f16": 4e4, "bf16": 5e6}[dtype]
+    z = rng.normal(0, 2, (8, V))
+    z[1] -= far
+    z[2] += far
+    z = torch.from_numpy(z.astype(np.float32)).to(TORCH[dtype])
+    info = torch.finfo(TORCH[dtype])
+    z[3] = info.min
+    z[4, V // 2:] = info.min
+    z[5] = info.max
+    z[6] = -float("inf")
+    z[7] = -float("inf")
+    z[7, 3] = info.min
+    z64, buf = z.double().numpy(), z.to(DEV)
+    at, sums = np.tile(np.array([0, 3, 5, -1], np.int32), (8, 1)), answers(rng, 8, 4, 2)
+    d = R.Distill(z64, at, sums, 2, T)
+    _, lse, grad = run_distill(buf, dtype, V, at, sums, 2, T)
+    within(grad, d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+    back = run_distill(buf, dtype, V, at, sums, 2, T, lse=lse)
+    kept = R.Distill(z64, at, sums, 2, T, lse=lse)
+    near = np.abs(lse) < 32768                                      # there the lse counts as it is given
+    assert near[[0, 4]].all() and not near[6] and (near[[3, 5]] == (info.max / T < 32768)).all()
+    within(back[near], kept.grad[near], kept.stored_error(HALF_STEP[dtype], LEAST[dtype])[near])
+    within(back[~near], d.grad[~near], d.stored_error(HALF_STEP[dtype], LEAST[dtype])[~near])
