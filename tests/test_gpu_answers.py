@@ -691,3 +691,55 @@ def test_gradient_alone_of_rows_far_from_zero(T, V, dtype):
     assert near[[0, 4]].all() and not near[6] and (near[[3, 5]] == (info.max / T < 32768)).all()
     within(back[near], kept.grad[near], kept.stored_error(HALF_STEP[dtype], LEAST[dtype])[near])
     within(back[~near], d.grad[~near], d.stored_error(HALF_STEP[dtype], LEAST[dtype])[~near])
+
+
+# ---- the longest rows where they are many -----------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,V,pad", [("f32", 66001, 0), ("f32", 40003, 1), ("f16", 131077, 0), ("f16", 66003, 1), ("bf16", 70001, 0)])
+def test_many_long_rows(dtype, V, pad):
+    """More rows than are cut into parts, of all that a workgroup holds and of more: ordinary ones, logits that rise and fall along
+    the row, logits far from 0 and masked ones, among padding.  Every row of some kind against the formulas."""
+    rng = np.random.default_rng(V)
+    rows, k, members = 131, 21, 3
+    far = {"f32": 5e6, "f16": 4e4, "bf16": 5e6}[dtype]
+    z = rng.normal(0, 2, (rows, V)).astype(np.float32)
+    z[1] += np.linspace(-400, 400, V)
+    z[64] += np.linspace(400, -400, V)
+    z[65] += far
+    z[66] -= far
+    z[67, V // 3:] = torch.finfo(TORCH[dtype]).min
+    z[68] = -np.inf
+    z[68, V - 2] = 1
+    z[69, :V - 5] = -np.inf
+    z[70] = -np.inf
+    use = [0, 1, 63, 64, 65, 66, 67, 68, 69, 70, 71, 129, 130]
+    buf = torch.full((rows, V + pad), float("nan"), dtype=TORCH[dtype], device=DEV)
+    buf[:, :V] = torch.from_numpy(z).to(TORCH[dtype]).to(DEV)
+    z = buf[use, :V].double().cpu().numpy()
+    index, sums = slots(rng, rows, V, k, empty=0.1), answers(rng, rows, k, members)
+    index[68, :] = V - 2                                            # an excluded class would cost an infinite loss
+    index[69, :5] = np.arange(V - 5, V)
+    index[69, 5:] = -1
+    index[67] %= V // 3
+    weight = np.full(rows, 0.5, np.float32)
+    weight[2:60:3] = 0
+    top, lp = run_top(buf, dtype, V, k)
+    want, wlp = R.top_logprobs(z, k)
+    assert np.array_equal(top[use], want)
+    within(lp[use], wlp, R.logprob_error(z, wlp))
+    at = run_at(buf, dtype, V, index)[use]
+    want = R.logprobs_at(z, index[use])
+    gone = want == -np.inf
+    assert np.array_equal(at == -np.inf, gone)
+    within(at[~gone], want[~gone], R.logprob_error(z, np.where(gone, 0.0, want))[~gone])
+    for T in (1.0, 0.5):
+        d = R.Distill(z, index[use], sums[use], members, T, weight[use])
+        loss, lse, grad = run_distill(buf, dtype, V, index, sums, members, T, weight)
+        within(loss[use], d.loss, d.loss_error)
+        finite = np.isfinite(d.lse)
+        within(lse[use][finite], d.lse[finite], d.lse_error[finite])
+        assert np.array_equal(lse[use][~finite], d.lse[~finite])
+        within(grad[use], d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
+        loss2, _, _ = run_distill(buf, dtype, V, index, sums, members, T, weight, grad=False)
+        within(loss2[use], d.loss, d.loss_error)
+        assert (loss[2:60:3] == 0).all() and (lse[2:60:3] == 0).all() and (grad[2:60:3] == 0).all()
