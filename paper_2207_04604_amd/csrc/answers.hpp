@@ -862,8 +862,10 @@ __global__ void __launch_bounds__(Group<NT>::SIZE) k_top(Rows in, uint32_t k, in
     top_of_row<T, NT, NV>(in, k, index, out);
 }
 
-// 512 and 1024 threads, as many such workgroups to a unit as make eight wavefronts a SIMD: that leaves each no more than 80 of
-// the scalar registers that the compiler may give it (64 of 2048 x 65536 in bf16 with 93 of them: 84 us instead of 64).
+// 512 and 1024 threads of up to 8 words: with no more than 64 vector and 80 scalar registers to a wavefront a SIMD holds eight of
+// them, two rows of up to 8192 words to a unit.  The vector registers come out so by themselves (float16 with 512 threads takes 70:
+// seven wavefronts), the scalar ones are capped (64 of 2048 x 65536 in bf16 with 93 of them: 84 us instead of 64).  1024
+// threads of 16 words take 93 vector registers: one row to a unit.
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(NT) __attribute__((amdgpu_num_sgpr(80))) k_top_long(Rows in, uint32_t k, int32_t *index, float *out)
 {
