@@ -57,9 +57,12 @@ template <class F> d2mhe_status with_type(uint32_t dtype, F f)
 }
 
 // Rows are cut into parts where 1024 threads would share one (beyond 8192 words) and up to 128 rows leave half of the units
-// without: whole / in parts, us: step of 64 x 131072 in f32 33.9 / 21.5, of 128 41.2 / 43.5; loss of 128 22.8 / 18.4; with up to
-// 8192 words the second launch costs more than it brings (step of 16 x 32768 in f32 8.1 / 10.4).  1024 workgroups instead of
-// 512: 64 x 131072 25.8 -> 21.5.  A part has 4 words for each of 256 threads.
+// without.  Whole / in parts, us, 131072 classes: step of 64 rows in f32 35.5 / 22.5, of 96 39.3 / 32.6, of 128 42.3 / 43.8, of 128 in
+// bf16 26.0 / 24.0; loss of 128 in f32 22.8 / 18.5, log-probabilities 20.7 / 17.0; 10^6 classes, step of 128 in f32 400 / 323.  One
+// limit for all, as there is one size of scratch for all; next to both borders it loses: step of 128 x 40000 in f32 16.4 / 16.9, its
+// loss 8.0 / 9.2, log-probabilities of 128 x 70000 in bf16 7.1 / 8.4.  With up to 8192 words the second launch costs more than it
+// brings (step of 16 x 32768 in f32 8.1 / 10.4).  1024 workgroups instead of 512: step of 64 x 131072 25.8 -> 21.5.  A part has 4
+// words for each of 256 threads.
 constexpr uint32_t SPLIT_ROWS = 128, SPLIT_WORDS = 8192, SPLIT_GROUPS = 1024, PART_WORDS = 1024;
 
 template <class T> uint32_t words_of(const d2mhe_logits *z) { return (z->classes + Pack<T>::E - 1) / Pack<T>::E; }

@@ -2,9 +2,11 @@
 // row, log-probabilities at given classes, distillation loss and gradient.
 //
 // All of them stream: a row of V logits is read once (and its gradient written once), with one exp2 per logit for the
-// statistics and one more for the gradient, 5 to 9 vector instructions a logit in all.  What bounds long rows is memory
-// (a device copy moves 4.9 TB/s here), short rows the instructions around a row.  Rows therefore stay in registers
-// between the passes, and 16 to 1024 threads share one: as many as hold it.
+// statistics and one more for the gradient.  Vector instructions a logit, by counters: log-probabilities of 32768 classes 9, loss of
+// 50001 10, top classes of 131072 11 and of 100 71, step of 131072 13 and of 32768 17, gradient alone of 1000 and of 65537 21: the
+// slots' part of the last is as large as the row's.  What bounds long rows is memory (a device copy moves 4.9 TB/s here), short rows
+// the instructions around a row.  Rows therefore stay in registers between the passes, and 16 to 1024 threads share one: as many
+// as hold it.
 #pragma once
 #include <hip/hip_fp16.h>
 #include <hip/hip_runtime.h>
@@ -647,7 +649,7 @@ template <class T, int NT, int NV, int BITS, class R, class Key> __device__ uint
 // Two rounds over a row in registers.  The first gives the maximum of every thread; the `each`-th largest of a wavefront's
 // maxima, the least of them over the wavefronts, is a bound that at least k elements reach.  (Few words or many slots: the
 // bound comes from the elements themselves.)  The second collects what reaches it, usually little more than k, in LDS, where
-// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 250 us, 4.3 TB/s (185 without the
+// every candidate counts the larger ones: that is its place.  64 of 4096 x 131072 in bf16: 252 us, 4.3 TB/s (185 without the
 // second round); vector ALU three quarters busy.  5 of 65536 x 100 in f16: 12 us, bound by its instructions.  (Four lanes to a
 // candidate: 261 us; the next row's words requested as this row's are looked through: 302, the compiler keeps both.)
 template <class T, int NT, int NV> __device__ __forceinline__ void top_of_row(const Rows &in, uint32_t k, int32_t *index, float *out)
