@@ -289,7 +289,8 @@ typedef struct {
 
 /* Bytes of scratch that d2mhe_top_logprobs, d2mhe_logprobs_at and d2mhe_distill need for these logits
  * and k (a positive multiple of 256; 0 if the descriptor is invalid; its pointer is not looked at).
- * Calls that overlap in time need a scratch each, graphs that are replayed side by side as well. */
+ * Calls that overlap in time need a scratch each, graphs that are replayed side by side as well.
+ * d2mhe_top_logprobs asks for it like the others and leaves it as it is.                          */
 size_t d2mhe_logits_scratch_bytes(const d2mhe_logits *z, uint32_t k);
 /* The k largest logits of every row in decreasing order (among equals the lower class first; -0 and
  * +0 are equal), index [rows][k], and their log-probabilities z - log sum exp z, logprob [rows][k].
@@ -298,7 +299,8 @@ d2mhe_status d2mhe_top_logprobs(const d2mhe_logits *z, uint32_t k, int32_t *inde
                                 void *scratch, size_t scratch_bytes, void *stream);
 /* logprob [rows][k] = z - log sum exp z at the classes index [rows][k], in any order, any of them more
  * than once; 0 in empty slots (an index outside 0 .. classes - 1).  The log-probability of a -inf
- * logit is -inf, which the encoders clamp to their least value.                                  */
+ * logit is -inf, which the encoders clamp to their least value; the NaN of a row with a NaN or +inf
+ * they encode as 0, a certain answer: such a row has to be kept out by the caller.                */
 d2mhe_status d2mhe_logprobs_at(const d2mhe_logits *z, const int32_t *index, uint32_t k, float *logprob,
                                void *scratch, size_t scratch_bytes, void *stream);
 /* Distillation towards the mean answer s_j = sum_j / members of the filled slots j of a row, at
