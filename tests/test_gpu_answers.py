@@ -686,7 +686,8 @@ def test_gradient_alone_of_rows_far_from_zero(T, V, dtype):
     _, lse, grad = run_distill(buf, dtype, V, at, sums, 2, T)
     within(grad, d.grad, d.stored_error(HALF_STEP[dtype], LEAST[dtype]))
     back = run_distill(buf, dtype, V, at, sums, 2, T, lse=lse)
-    kept = R.Distill(z64, at, sums, 2, T, lse=lse)
+    with np.errstate(invalid="ignore"):                             # rows that have no finite lse, and are not compared
+        kept = R.Distill(z64, at, sums, 2, T, lse=lse)
     near = np.abs(lse) < 32768                                      # there the lse counts as it is given
     assert near[[0, 4]].all() and not near[6] and (near[[3, 5]] == (info.max / T < 32768)).all()
     within(back[near], kept.grad[near], kept.stored_error(HALF_STEP[dtype], LEAST[dtype])[near])
